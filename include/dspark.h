@@ -17,7 +17,9 @@
  * Upstream of them, the drafter's sequential stage (dspark_markov_draft,
  * dspark_rnn_draft) produces the draft tokens, distributions and confidences
  * they consume; dspark_check_*_inputs look at a call's device-side values
- * before it.
+ * before it.  Around the step, the paged KV cache: dspark_cache_append and
+ * dspark_verify_attn_scaled write and read it in 8 bits, dspark_pages_* hand
+ * out, share, take back and move its pages.
  *
  * Conventions shared by every entry point
  *   - All array arguments are DEVICE pointers unless marked "host".  Arrays are
@@ -229,6 +231,157 @@ dspark_status dspark_verify_attn(const void* q, const void* k_cache, const void*
                                  size_t ws_bytes, dspark_stream stream);
 
 /* ------------------------------------------------------------------------
+ * The paged cache in 8 bits.  Keys and values are e4m3 codes (sign, four
+ * exponent bits of bias 7, three fraction bits; at most 448, 0x7f is NaN), one
+ * byte each, laid out as dspark_verify_attn's caches with strides in bytes.
+ * `block` tokens of a page and a head share an fp32 scale, keys and values
+ * apart: code * scale is the value.
+ *   k_scale, v_scale  [num_pages, Hkv, page_size / block] fp32, dense.
+ *   block       a multiple of 16 that divides page_size.
+ *   num_pages   pages of the cache.
+ *
+ * dspark_cache_append quantises the rows of a step (or of a prompt) into the
+ * cache: row cu_q[r] + t of request r is token kv_len_r - q_len_r + t, so a
+ * step's rows are written before dspark_verify_attn_scaled reads them with the
+ * same kv_len, cu_q and block_table.
+ *   k           [total_q, Hkv, Dqk] new keys in dt, a row every k_ld elements
+ *               (k_ld >= Hkv * Dqk: rows may be a part of a wider projection).
+ *   v           [total_q, Hkv, Dv], likewise with v_ld.  NULL, with v_cache and
+ *               v_scale NULL: keys alone (a latent cache, whose values are a
+ *               part of its keys; v_strides and Dv are not looked at).
+ *   For every block that gets tokens: scale = the smallest power of two s with
+ *   max |x| <= 448 s over its new finite values, and not below the scale that
+ *   its earlier tokens have (rounded up to a power of two); exponent in
+ *   [-100, 120]; 1 where all are 0.  code = e4m3(x / s), to nearest even; a
+ *   value that is not finite becomes NaN.  Where the scale grows the earlier
+ *   tokens' codes become e4m3(code * old / s), exact down to 2^-6 of s.  Tokens
+ *   behind the new ones, and other blocks, stay as they are.
+ *   max_q       host bound on every q_len_r, up to 2^20.  A request is skipped
+ *               under the rules of dspark_verify_attn; a block whose page is
+ *               outside [0, num_pages) is not written.
+ *   Two requests whose new tokens lie on the same page must not be in one call
+ *   (dspark_pages_reserve copies such pages first).
+ *   Limits: R <= 8192, Dqk, Dv multiples of 8 up to 576, page_size a multiple
+ *   of 16, max_pages * page_size <= 2^30.  Rows and slots are read and written 8
+ *   values at a time where k, v and their rows are 16-byte and the caches and
+ *   their strides 8-byte aligned, else one at a time.
+ *
+ * dspark_verify_attn_scaled is dspark_verify_attn over such a cache: the same
+ * arguments, rules, outputs and limits (dt: queries and output; the softmax in
+ * fp32).  Table entries outside [0, num_pages) read the nearest page inside.
+ * v_cache may alias k_cache, with v_scale = k_scale.
+ *   ws of dspark_verify_attn_scaled_workspace_size bytes, 256-aligned; a smaller
+ *   one is refused (DSPARK_EWORKSPACE).  A non-finite key, value or scale
+ *   reaches only the rows that see it.
+ * ---------------------------------------------------------------------- */
+dspark_status dspark_cache_append(const void* k, const void* v, int64_t k_ld, int64_t v_ld,
+                                  dspark_dtype dt, void* k_cache, void* v_cache,
+                                  const int64_t* k_strides, const int64_t* v_strides, float* k_scale,
+                                  float* v_scale, int block, const int32_t* block_table,
+                                  int max_pages, int num_pages, const int32_t* kv_len,
+                                  const int32_t* cu_q, int R, int max_q, int Hkv, int Dqk, int Dv,
+                                  int page_size, dspark_stream stream);
+
+size_t dspark_verify_attn_scaled_workspace_size(int R, int max_q, int Hq, int Hkv, int Dqk, int Dv,
+                                                int max_pages, int page_size, int block,
+                                                dspark_dtype dt);
+
+dspark_status dspark_verify_attn_scaled(const void* q, const void* k_cache, const void* v_cache,
+                                        const int64_t* k_strides, const int64_t* v_strides,
+                                        const float* k_scale, const float* v_scale, int block,
+                                        const int32_t* block_table, int max_pages, int num_pages,
+                                        const int32_t* kv_len, const int32_t* cu_q, int R, int max_q,
+                                        int Hq, int Hkv, int Dqk, int Dv, int page_size, float scale,
+                                        dspark_dtype dt, void* out, float* lse, void* ws,
+                                        size_t ws_bytes, dspark_stream stream);
+
+/* ------------------------------------------------------------------------
+ * The pages of a paged cache (of any element type): handing out, sharing,
+ * taking back and moving.  The state, all in device memory:
+ *   block_table [R, max_pages] int32, kv_len [R] int32: as dspark_verify_attn
+ *               reads them.  Request r holds its first ceil(kv_len_r /
+ *               page_size) table entries; entries past them mean nothing.  A row
+ *               of length 0 is a free place for a request.
+ *   ref         [num_pages] int32: how many held entries name the page; 0: free.
+ * Every result is a function of the inputs (no order of atomics shows).  The
+ * calls change the state in the order of their stream and never wait for the
+ * host, so a step may be captured in a graph.
+ *   bufs        host array of the memory that pages are made of: page p of a
+ *               buffer is the page_bytes bytes at base + p * page_stride (base
+ *               device memory; keys, values, scales, layer by layer).  The array
+ *               is read during the call only.  At most 1024, page_stride at most
+               2^31; n_bufs 0 copies nothing.
+ *   ws          dspark_pages_workspace_size(R, num_pages) bytes, 256-aligned.
+ *
+ * dspark_pages_reserve: pages for cu_q[r+1] - cu_q[r] more tokens of every
+ *   request.  Requests are served in order as far as the free pages go: a
+ *   request is served when the pages that it and all requests before it need
+ *   are there, or when it needs none.  Free pages are taken lowest ids first.
+ *   Where a request's last page is partly filled and others hold it too, it
+ *   gets a copy (in every buffer) before it grows; when all holders of a page
+ *   grow in the call, the last of them keeps it.
+ *   step_len    [R] int32 out: kv_len_r + q_len_r, the kv_len of the step's
+ *               dspark_cache_append and attention; 0 where the request was not
+ *               served (they skip it) or its values are malformed (kv_len_r or
+ *               the sum outside [0, max_pages * page_size], q_len_r negative, a
+ *               partly filled last page outside the cache).  kv_len stays as it
+ *               is.  step_len must not be kv_len.
+ * dspark_pages_commit: after the step, request r keeps 1 + accepted_len_r of
+ *   its q_len_r tokens (within [0, q_len_r]; accepted_len NULL: all of them):
+ *   kv_len_r = step_len_r - q_len_r + kept, and the pages past it are given
+ *   back.  Requests with step_len_r outside [1, max_pages * page_size] or q_len_r
+ *   outside [0, step_len_r] are left as they are.
+ * dspark_pages_trim: kv_len_r = min(kv_len_r, max(new_len_r, 0)), and the pages
+ *   past it are given back; new_len_r = 0 ends the request.  A page cut inside
+ *   stays shared with its other holders; reserve copies it.
+ * dspark_pages_fork: for i < n, request child[i] (of length 0) gets the first
+ *   min(kv_len, len[i]) tokens (len NULL: all) of request parent[i], by sharing
+ *   its pages.  Lengths are those before the call.  A pair is skipped when
+ *   parent or child is outside [0, R), they are the same, the child's length is
+ *   not 0, or an earlier pair names the same child.  n <= R.
+ * dspark_pages_compact: moves the pages in use to ids 0 .. *used - 1: the k-th
+ *   used page from *used on, in every buffer, to the k-th free page below it;
+ *   held table entries and ref follow.  *used (device int32): pages in use.
+ *   Contents of the pages that become free stay what they were.
+ *   Limits: 1 <= R <= 8192, page_size a multiple of 16, max_pages * page_size
+ *   <= 2^30, 1 <= num_pages <= 2^24.  Table entries outside [0, num_pages) are
+ *   passed over, so no access leaves the buffers; dspark_check_page_inputs looks
+ *   at the state.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    void* base;
+    int64_t page_stride; /* bytes, >= page_bytes */
+    int64_t page_bytes;
+} dspark_page_buffer;
+
+size_t dspark_pages_workspace_size(int R, int num_pages);
+
+dspark_status dspark_pages_reserve(int32_t* block_table, int max_pages, const int32_t* kv_len,
+                                   const int32_t* cu_q, int R, int page_size, int32_t* ref,
+                                   int num_pages, const dspark_page_buffer* bufs, int n_bufs,
+                                   int32_t* step_len, void* ws, size_t ws_bytes,
+                                   dspark_stream stream);
+
+dspark_status dspark_pages_commit(const int32_t* block_table, int max_pages, int32_t* kv_len,
+                                  const int32_t* step_len, const int32_t* cu_q,
+                                  const int32_t* accepted_len, int R, int page_size, int32_t* ref,
+                                  int num_pages, dspark_stream stream);
+
+dspark_status dspark_pages_trim(const int32_t* block_table, int max_pages, int32_t* kv_len,
+                                const int32_t* new_len, int R, int page_size, int32_t* ref,
+                                int num_pages, dspark_stream stream);
+
+dspark_status dspark_pages_fork(int32_t* block_table, int max_pages, int32_t* kv_len, int R,
+                                int page_size, int32_t* ref, int num_pages, const int32_t* parent,
+                                const int32_t* child, const int32_t* len, int n, void* ws,
+                                size_t ws_bytes, dspark_stream stream);
+
+dspark_status dspark_pages_compact(int32_t* block_table, int max_pages, const int32_t* kv_len, int R,
+                                   int page_size, int32_t* ref, int num_pages,
+                                   const dspark_page_buffer* bufs, int n_bufs, int32_t* used,
+                                   void* ws, size_t ws_bytes, dspark_stream stream);
+
+/* ------------------------------------------------------------------------
  * Stage 3: speculative acceptance (the background section on speculative
  * decoding: left-to-right test, first rejection discards the suffix, one
  * corrected or bonus token per round).
@@ -394,11 +547,20 @@ dspark_status dspark_rnn_draft(const int32_t* anchor, const void* base_logits,
  * sts_temp (nullable), R, K): code 1 a temperature sts_temp[k] not finite and
  * positive (request -1, index k, value: the float's bits); 2 u[r, k] outside
  * [0, 1) or NaN (index k, value: the float's bits).
+ * dspark_check_page_inputs (the state of dspark_pages_*): code 1 kv_len_r
+ * outside [0, max_pages*page_size] (value kv_len_r); 2 a table entry that
+ * request r holds outside [0, num_pages) (index: logical page, value: the
+ * entry); 3 one that names a page with ref below 1 (likewise).
  * ---------------------------------------------------------------------- */
 dspark_status dspark_check_verify_inputs(const int32_t* block_table, int max_pages,
                                          const int32_t* kv_len, const int32_t* cu_q, int R,
                                          int max_q, int page_size, int num_pages, int32_t* report,
                                          dspark_stream stream);
+
+dspark_status dspark_check_page_inputs(const int32_t* block_table, int max_pages,
+                                       const int32_t* kv_len, int R, int page_size,
+                                       const int32_t* ref, int num_pages, int32_t* report,
+                                       dspark_stream stream);
 
 dspark_status dspark_check_accept_inputs(const int32_t* cu_q, const float* u, int R, int K,
                                          int32_t* report, dspark_stream stream);

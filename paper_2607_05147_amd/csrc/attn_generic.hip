@@ -1,6 +1,7 @@
 // Ragged causal verify attention over a paged KV cache, vector-ALU path.
 //
-// Handles fp32 and bf16 and any head size that is a multiple of 8 (up to 576),
+// Handles fp32 and bf16 (and caches of e4m3 codes with a scale for each block of
+// tokens and head) and any head size that is a multiple of 8 (up to 576),
 // any alignment, and latent attention where the values alias the keys: what the
 // matrix-core kernels do not take (unaligned buffers or strides, head sizes above
 // 256 other than the latent shape on pages of 64 and more).  One wave per
@@ -10,6 +11,7 @@
 // Every split writes (max, sum, unnormalised output) for its rows; a merge
 // kernel combines the splits in order, so results are bitwise reproducible.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.h"
 #include "kernels.h"
@@ -40,7 +42,20 @@ struct GenParams {
     int group;
     float scale2; // scale * log2(e)
     float* part;  // [R*max_q][Hq][splits][Dv + 2]
+    CacheScales cs;  // caches of e4m3 codes only
 };
+
+// A cache of e4m3 codes: key j of a request is on this page, and the index of its scale.
+struct E4m3 {};
+template <> struct Elem<E4m3> {
+    __device__ __forceinline__ static float load(const E4m3* p, int64_t i) { return e4m3_to_f32(((const uint8_t*)p)[i]); }
+};
+static_assert(sizeof(E4m3) == 1, "a code is a byte");
+__device__ __forceinline__ int64_t scaled_page(const GenParams& p, const int32_t* bt, int j, int g, int64_t& at) {
+    const int64_t page = min(max(bt[j / p.a.page], 0), p.cs.num_pages - 1);
+    at = (page * p.a.Hkv + g) * (p.a.page / p.cs.block) + j % p.a.page / p.cs.block;
+    return page;
+}
 
 // flattened verify tokens, clamped to the R * max_q rows the caller sized for
 __device__ __forceinline__ int cu_q_total(const AttnArgs& a) {
@@ -62,8 +77,10 @@ __device__ __forceinline__ bool gen_request(const AttnArgs& a, int r, int& q0, i
     return q0 >= 0 && (int64_t)q0 + ql <= cu_q_total(a);
 }
 
-template <typename T>
+// T: queries and output; C: the cache (T, or E4m3)
+template <typename T, typename C>
 __global__ __launch_bounds__(DSPARK_WAVE) void attn_generic_kernel(GenParams p) {
+    constexpr bool kScaled = std::is_same<C, E4m3>::value;
     const AttnArgs& a = p.a;
     __shared__ float qs[kGenHB][kGenMaxD];
     const int lane = threadIdx.x;
@@ -86,8 +103,8 @@ __global__ __launch_bounds__(DSPARK_WAVE) void attn_generic_kernel(GenParams p) 
     const int k_end = min(visible, k_begin + per);
 
     const T* q = (const T*)a.q;
-    const T* kc = (const T*)a.k;
-    const T* vc = (const T*)a.v;
+    const C* kc = (const C*)a.k;
+    const C* vc = (const C*)a.v;
     for (int i = lane; i < kGenHB * a.Dqk; i += DSPARK_WAVE) {
         const int hh = i / a.Dqk, d = i % a.Dqk;
         qs[hh][d] = hh < nh ? Elem<T>::load(q, ((int64_t)tok * a.Hq + h0 + hh) * a.Dqk + d) *
@@ -112,12 +129,18 @@ __global__ __launch_bounds__(DSPARK_WAVE) void attn_generic_kernel(GenParams p) 
 #pragma unroll
         for (int hh = 0; hh < kGenHB; ++hh) sc[hh] = 0.0f;
         if (valid) {
-            const int64_t page = bt[j / a.page];
-            const T* kr = kc + page * a.ks[0] + g * a.ks[1] + (int64_t)(j % a.page) * a.ks[2];
+            int64_t at = 0;
+            const int64_t page = kScaled ? scaled_page(p, bt, j, g, at) : bt[j / a.page];
+            const C* kr = kc + page * a.ks[0] + g * a.ks[1] + (int64_t)(j % a.page) * a.ks[2];
             for (int d = 0; d < a.Dqk; ++d) {
-                const float kd = Elem<T>::load(kr, d);
+                const float kd = Elem<C>::load(kr, d);
 #pragma unroll
                 for (int hh = 0; hh < kGenHB; ++hh) sc[hh] += qs[hh][d] * kd;
+            }
+            if constexpr (kScaled) {
+                const float ks = p.cs.k[at];
+#pragma unroll
+                for (int hh = 0; hh < kGenHB; ++hh) sc[hh] *= ks;
             }
         }
         float pr[kGenHB];
@@ -136,16 +159,22 @@ __global__ __launch_bounds__(DSPARK_WAVE) void attn_generic_kernel(GenParams p) 
         const int nvalid = min(DSPARK_WAVE, k_end - k0);
         for (int jj = 0; jj < nvalid; ++jj) {
             const int key = k0 + jj;
-            const int64_t page = bt[key / a.page];
-            const T* vr = vc + page * a.vs[0] + g * a.vs[1] + (int64_t)(key % a.page) * a.vs[2];
+            int64_t at = 0;
+            const int64_t page = kScaled ? scaled_page(p, bt, key, g, at) : bt[key / a.page];
+            const C* vr = vc + page * a.vs[0] + g * a.vs[1] + (int64_t)(key % a.page) * a.vs[2];
             float pj[kGenHB];
 #pragma unroll
             for (int hh = 0; hh < kGenHB; ++hh) pj[hh] = __shfl(pr[hh], jj, DSPARK_WAVE);
+            if constexpr (kScaled) {
+                const float vs = p.cs.v[at];
+#pragma unroll
+                for (int hh = 0; hh < kGenHB; ++hh) pj[hh] *= vs;
+            }
 #pragma unroll
             for (int e = 0; e < kGenDPL; ++e) {
                 const int d = lane + e * DSPARK_WAVE;
                 if (d < a.Dv) {
-                    const float vd = Elem<T>::load(vr, d);
+                    const float vd = Elem<C>::load(vr, d);
 #pragma unroll
                     for (int hh = 0; hh < kGenHB; ++hh) o[hh][e] += pj[hh] * vd;
                 }
@@ -196,7 +225,9 @@ __global__ __launch_bounds__(256) void attn_generic_merge(GenParams p) {
     if (a.lse && threadIdx.x == 0) a.lse[row] = (M + log2f(L)) * kLn2;
 }
 
-hipError_t launch_attn_generic(const AttnArgs& a, void* ws, hipStream_t s) {
+namespace {
+
+hipError_t launch_generic(const AttnArgs& a, const CacheScales* cs, void* ws, hipStream_t s) {
     GenParams p;
     p.a = a;
     p.splits = gen_splits(a);
@@ -204,14 +235,14 @@ hipError_t launch_attn_generic(const AttnArgs& a, void* ws, hipStream_t s) {
     p.nhb = (p.group + kGenHB - 1) / kGenHB;
     p.scale2 = a.scale * kLog2e;
     p.part = (float*)ws;
+    p.cs = cs ? *cs : CacheScales{};
     const int64_t tokens = (int64_t)a.R * a.max_q;
     const int64_t items = tokens * a.Hkv * p.nhb * p.splits;
-    if (a.bf16)
-        hipLaunchKernelGGL(attn_generic_kernel<uint16_t>, dim3((unsigned)items), dim3(DSPARK_WAVE),
-                           0, s, p);
-    else
-        hipLaunchKernelGGL(attn_generic_kernel<float>, dim3((unsigned)items), dim3(DSPARK_WAVE), 0,
-                           s, p);
+    const dim3 grid((unsigned)items), wave(DSPARK_WAVE);
+    if (cs && a.bf16) hipLaunchKernelGGL((attn_generic_kernel<uint16_t, E4m3>), grid, wave, 0, s, p);
+    else if (cs) hipLaunchKernelGGL((attn_generic_kernel<float, E4m3>), grid, wave, 0, s, p);
+    else if (a.bf16) hipLaunchKernelGGL((attn_generic_kernel<uint16_t, uint16_t>), grid, wave, 0, s, p);
+    else hipLaunchKernelGGL((attn_generic_kernel<float, float>), grid, wave, 0, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t rows = tokens * a.Hq;
@@ -220,6 +251,14 @@ hipError_t launch_attn_generic(const AttnArgs& a, void* ws, hipStream_t s) {
     else
         hipLaunchKernelGGL(attn_generic_merge<float>, dim3((unsigned)rows), dim3(256), 0, s, p);
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_generic(const AttnArgs& a, void* ws, hipStream_t s) { return launch_generic(a, nullptr, ws, s); }
+
+hipError_t launch_attn_generic_scaled(const AttnArgs& a, const CacheScales& c, void* ws, hipStream_t s) {
+    return launch_generic(a, &c, ws, s);
 }
 
 }  // namespace dspark

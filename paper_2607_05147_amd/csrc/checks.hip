@@ -177,6 +177,44 @@ __global__ __launch_bounds__(kChkThreads) void chk_draft(const float* u, const f
     if (!done && threadIdx.x == 0) report[0] = report[1] = report[2] = report[3] = 0;
 }
 
+// Page state: 1 kv_len outside [0, max_pages*page_size]; 2 a table entry of a page the
+// request holds outside [0, num_pages) (index: logical page, value: the entry); 3 one that
+// names a page without holders (ref below 1).
+__global__ __launch_bounds__(kChkThreads) void chk_pages(const int32_t* block_table, int max_pages,
+                                                         const int32_t* kv_len, int R, int page_size,
+                                                         const int32_t* ref, int num_pages, int32_t* report) {
+    bool done = false;
+    for (int base = 0; base < R && !done; base += kChkThreads) {
+        const int r = base + (int)threadIdx.x;
+        Finding f{0, r, 0, 0};
+        if (r < R) {
+            const int kv = kv_len[r];
+            if (kv < 0 || (int64_t)kv > (int64_t)max_pages * page_size) {
+                f = Finding{1, r, 0, kv};
+            } else {
+                const int np = (int)(((int64_t)kv + page_size - 1) / page_size);
+                for (int p = 0; p < np; ++p) {
+                    const int e = block_table[(int64_t)r * max_pages + p];
+                    const bool in = e >= 0 && e < num_pages;
+                    if (!in || ref[e] < 1) {
+                        f = Finding{in ? 3 : 2, r, p, e};
+                        break;
+                    }
+                }
+            }
+        }
+        report_first(f, report, done);
+    }
+    if (!done && threadIdx.x == 0) report[0] = report[1] = report[2] = report[3] = 0;
+}
+
+hipError_t launch_check_pages(const int32_t* block_table, int max_pages, const int32_t* kv_len, int R, int page_size,
+                              const int32_t* ref, int num_pages, int32_t* report, hipStream_t s) {
+    hipLaunchKernelGGL(chk_pages, dim3(1), dim3(kChkThreads), 0, s, block_table, max_pages, kv_len, R, page_size, ref,
+                       num_pages, report);
+    return hipGetLastError();
+}
+
 hipError_t launch_check_draft(const float* u, const float* sts_temp, int R, int K, int32_t* report,
                               hipStream_t s) {
     hipLaunchKernelGGL(chk_draft, dim3(1), dim3(kChkThreads), 0, s, u, sts_temp, R, K, report);

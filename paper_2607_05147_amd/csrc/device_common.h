@@ -34,6 +34,10 @@ template <> struct Elem<uint16_t> {
     }
 };
 
+// The value of an e4m3 code (four significant bits, exponents from -6, at most
+// 448; 0x7f is NaN), the low byte of `b`.
+__device__ __forceinline__ float e4m3_to_f32(uint32_t b) { return __builtin_amdgcn_cvt_f32_fp8(b, 0); }
+
 // Wave-wide reductions over 64 lanes (every lane gets the result).
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll

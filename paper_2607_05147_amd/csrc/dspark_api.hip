@@ -43,6 +43,9 @@ constexpr int kMaxSchedCand = 8192;
 constexpr int kMaxR = 8192;
 constexpr int kMaxD = 576;
 constexpr int kMaxV = 1 << 20;
+constexpr int kMaxAppend = 1 << 20;  // rows of a request that are appended in one call
+constexpr int kMaxPages = 1 << 24;
+constexpr int kMaxBufs = 1024;       // buffers that a cache's pages are made of
 
 dspark::AttnArgs make_attn(const void* q, const void* k_cache, const void* v_cache,
                            const int64_t* k_strides, const int64_t* v_strides,
@@ -338,6 +341,250 @@ dspark_status dspark_verify_attn(const void* q, const void* k_cache, const void*
                       : path == 2 ? dspark::launch_attn_stream(a, ws, s)
                                   : dspark::launch_attn_generic(a, ws, s),
                       "dspark_verify_attn");
+}
+
+// ------------------------------------------------------------------ the cache in 8 bits
+
+namespace {
+
+dspark_status check_block(int block, int page_size) {
+    if (block < 16 || block % 16 || page_size % block)
+        return fail(DSPARK_EUNSUPPORTED, "block=%d (a multiple of 16 that divides page_size=%d)", block, page_size);
+    return DSPARK_OK;
+}
+
+dspark_status check_strides(const int64_t* st, int D) {
+    for (int i = 0; i < 3; ++i)
+        if (st[i] < 0) return fail(DSPARK_EINVAL, "negative stride");
+    if (st[2] < D) return fail(DSPARK_ESHAPE, "token stride smaller than the head dim");
+    return DSPARK_OK;
+}
+
+}  // namespace
+
+dspark_status dspark_cache_append(const void* k, const void* v, int64_t k_ld, int64_t v_ld, dspark_dtype dt,
+                                  void* k_cache, void* v_cache, const int64_t* k_strides, const int64_t* v_strides,
+                                  float* k_scale, float* v_scale, int block, const int32_t* block_table, int max_pages,
+                                  int num_pages, const int32_t* kv_len, const int32_t* cu_q, int R, int max_q, int Hkv,
+                                  int Dqk, int Dv, int page_size, dspark_stream stream) {
+    const bool keys_alone = !v && !v_cache && !v_scale;
+    if (max_q < 1 || max_q > kMaxAppend) return fail(DSPARK_EINVAL, "max_q=%d outside [1, %d]", max_q, kMaxAppend);
+    // (the checks of the attention that reads the cache, whatever its queries' heads)
+    if (dspark_status st = check_attn_shape(R, 1, Hkv, Hkv, Dqk, keys_alone ? Dqk : Dv, max_pages, page_size, dt)) return st;
+    if (dspark_status st = check_block(block, page_size)) return st;
+    if (num_pages < 1) return fail(DSPARK_EINVAL, "num_pages=%d", num_pages);
+    if (!k || !k_cache || !k_strides || !k_scale || !block_table || !kv_len || !cu_q ||
+        (!keys_alone && (!v || !v_cache || !v_strides || !v_scale)))
+        return fail(DSPARK_EINVAL, "null argument");
+    if (dspark_status st = check_strides(k_strides, Dqk)) return st;
+    if (!keys_alone)
+        if (dspark_status st = check_strides(v_strides, Dv)) return st;
+    if (k_ld < (int64_t)Hkv * Dqk || (!keys_alone && v_ld < (int64_t)Hkv * Dv))
+        return fail(DSPARK_ESHAPE, "rows overlap: k_ld=%lld v_ld=%lld", (long long)k_ld, (long long)v_ld);
+    if ((int64_t)R * max_q > INT32_MAX) return fail(DSPARK_EUNSUPPORTED, "R*max_q=%lld too large", (long long)R * max_q);
+    const size_t esz = dt == DSPARK_BF16 ? 2 : 4;
+    if (!aligned(k, esz) || !aligned(v, esz) || !aligned(k_scale, 4) || !aligned(v_scale, 4) ||
+        !aligned(block_table, 4) || !aligned(kv_len, 4) || !aligned(cu_q, 4))
+        return fail(DSPARK_EINVAL, "misaligned pointer");
+    dspark::AppendArgs a = {};
+    a.k = k;
+    a.v = keys_alone ? nullptr : v;
+    a.k_ld = k_ld;
+    a.v_ld = v_ld;
+    a.bf16 = dt == DSPARK_BF16;
+    a.k_cache = k_cache;
+    a.v_cache = v_cache;
+    for (int i = 0; i < 3; ++i) {
+        a.ks[i] = k_strides[i];
+        a.vs[i] = keys_alone ? 0 : v_strides[i];
+    }
+    a.k_scale = k_scale;
+    a.v_scale = v_scale;
+    a.block = block;
+    a.block_table = block_table;
+    a.max_pages = max_pages;
+    a.num_pages = num_pages;
+    a.kv_len = kv_len;
+    a.cu_q = cu_q;
+    a.R = R;
+    a.max_q = max_q;
+    a.Hkv = Hkv;
+    a.Dqk = Dqk;
+    a.Dv = Dv;
+    a.page = page_size;
+    return hip_status(dspark::launch_cache_append(a, (hipStream_t)stream), "dspark_cache_append");
+}
+
+size_t dspark_verify_attn_scaled_workspace_size(int R, int max_q, int Hq, int Hkv, int Dqk, int Dv, int max_pages,
+                                                int page_size, int block, dspark_dtype dt) {
+    if (check_attn_shape(R, max_q, Hq, Hkv, Dqk, Dv, max_pages, page_size, dt) != DSPARK_OK ||
+        check_block(block, page_size) != DSPARK_OK)
+        return 0;
+    dspark::AttnArgs a = make_attn(nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, max_pages, nullptr, nullptr, R,
+                                   max_q, Hq, Hkv, Dqk, Dv, page_size, 1.0f, dt, nullptr, nullptr);
+    return dspark::attn_generic_workspace(a);
+}
+
+dspark_status dspark_verify_attn_scaled(const void* q, const void* k_cache, const void* v_cache,
+                                        const int64_t* k_strides, const int64_t* v_strides, const float* k_scale,
+                                        const float* v_scale, int block, const int32_t* block_table, int max_pages,
+                                        int num_pages, const int32_t* kv_len, const int32_t* cu_q, int R, int max_q,
+                                        int Hq, int Hkv, int Dqk, int Dv, int page_size, float scale, dspark_dtype dt,
+                                        void* out, float* lse, void* ws, size_t ws_bytes, dspark_stream stream) {
+    if (dspark_status st = check_attn_shape(R, max_q, Hq, Hkv, Dqk, Dv, max_pages, page_size, dt)) return st;
+    if (dspark_status st = check_block(block, page_size)) return st;
+    if (num_pages < 1) return fail(DSPARK_EINVAL, "num_pages=%d", num_pages);
+    if (!q || !k_cache || !v_cache || !k_strides || !v_strides || !k_scale || !v_scale || !block_table || !kv_len ||
+        !cu_q || !out)
+        return fail(DSPARK_EINVAL, "null argument");
+    if (dspark_status st = check_strides(k_strides, Dqk)) return st;
+    if (dspark_status st = check_strides(v_strides, Dv)) return st;
+    if (!isfinite(scale) || !(scale > 0.0f))
+        return fail(DSPARK_EINVAL, "scale=%g (must be finite and > 0)", (double)scale);
+    const size_t esz = dt == DSPARK_BF16 ? 2 : 4;
+    if (!aligned(q, esz) || !aligned(out, esz) || !aligned(lse, 4) || !aligned(k_scale, 4) || !aligned(v_scale, 4) ||
+        !aligned(block_table, 4) || !aligned(kv_len, 4) || !aligned(cu_q, 4))
+        return fail(DSPARK_EINVAL, "misaligned pointer");
+    const dspark::AttnArgs a = make_attn(q, k_cache, v_cache, k_strides, v_strides, block_table, max_pages, kv_len, cu_q,
+                                         R, max_q, Hq, Hkv, Dqk, Dv, page_size, scale, dt, out, lse);
+    const dspark::CacheScales c = {k_scale, v_scale, block, num_pages};
+    const size_t need = dspark::attn_generic_workspace(a);
+    if (ws_bytes < need || (need > 0 && !ws) || !aligned(ws, 256))
+        return fail(DSPARK_EWORKSPACE, "workspace of %zu bytes (256-aligned) needed, got %zu", need, ws_bytes);
+    return hip_status(dspark::launch_attn_generic_scaled(a, c, ws, (hipStream_t)stream), "dspark_verify_attn_scaled");
+}
+
+// ------------------------------------------------------------------ pages
+
+namespace {
+
+dspark_status check_page_sizes(int R, int max_pages, int page_size, int num_pages) {
+    if (R < 1 || R > kMaxR) return fail(DSPARK_EINVAL, "R=%d outside [1, %d]", R, kMaxR);
+    if (max_pages < 1 || num_pages < 1 || num_pages > kMaxPages)
+        return fail(DSPARK_EINVAL, "max_pages=%d num_pages=%d", max_pages, num_pages);
+    if (page_size < 16 || page_size % 16)
+        return fail(DSPARK_EUNSUPPORTED, "page_size=%d (need a multiple of 16)", page_size);
+    if ((int64_t)max_pages * page_size > (int64_t)1 << 30)
+        return fail(DSPARK_EUNSUPPORTED, "context bound max_pages*page_size too large");
+    return DSPARK_OK;
+}
+
+dspark_status check_page_ws(int R, int num_pages, const void* ws, size_t ws_bytes) {
+    const size_t need = dspark::pages_workspace(R, num_pages);
+    if (ws_bytes < need || !ws || !aligned(ws, 256))
+        return fail(DSPARK_EWORKSPACE, "workspace of %zu bytes (256-aligned) needed, got %zu", need, ws_bytes);
+    return DSPARK_OK;
+}
+
+// `n` (at most kMaxBufs) buffers, as the kernels take them
+dspark_status check_page_bufs(const dspark_page_buffer* bufs, int n, dspark::PageBuffer* to) {
+    if (n < 0 || n > kMaxBufs) return fail(DSPARK_EINVAL, "n_bufs=%d outside [0, %d]", n, kMaxBufs);
+    if (n > 0 && !bufs) return fail(DSPARK_EINVAL, "null bufs");
+    for (int i = 0; i < n; ++i) {
+        if (!bufs[i].base || bufs[i].page_bytes < 1) return fail(DSPARK_EINVAL, "buffer %d: null or empty", i);
+        if (bufs[i].page_stride < bufs[i].page_bytes || bufs[i].page_stride > (int64_t)1 << 31)
+            return fail(DSPARK_ESHAPE, "buffer %d: page_stride=%lld page_bytes=%lld", i, (long long)bufs[i].page_stride,
+                        (long long)bufs[i].page_bytes);
+        to[i] = dspark::PageBuffer{bufs[i].base, bufs[i].page_stride, bufs[i].page_bytes};
+    }
+    return DSPARK_OK;
+}
+
+dspark::PageArgs make_pages(const int32_t* block_table, int max_pages, const int32_t* kv_len, int R, int page_size,
+                            int32_t* ref, int num_pages) {
+    // (which of them a call writes is its own matter)
+    return dspark::PageArgs{const_cast<int32_t*>(block_table), max_pages, const_cast<int32_t*>(kv_len), R, page_size, ref,
+                            num_pages};
+}
+
+}  // namespace
+
+size_t dspark_pages_workspace_size(int R, int num_pages) {
+    if (R < 1 || R > kMaxR || num_pages < 1 || num_pages > kMaxPages) return 0;
+    return dspark::pages_workspace(R, num_pages);
+}
+
+dspark_status dspark_pages_reserve(int32_t* block_table, int max_pages, const int32_t* kv_len, const int32_t* cu_q, int R,
+                                   int page_size, int32_t* ref, int num_pages, const dspark_page_buffer* bufs, int n_bufs,
+                                   int32_t* step_len, void* ws, size_t ws_bytes, dspark_stream stream) {
+    if (dspark_status st = check_page_sizes(R, max_pages, page_size, num_pages)) return st;
+    if (!block_table || !kv_len || !cu_q || !ref || !step_len) return fail(DSPARK_EINVAL, "null argument");
+    if (step_len == kv_len) return fail(DSPARK_EINVAL, "step_len is kv_len");
+    if (!aligned(block_table, 4) || !aligned(kv_len, 4) || !aligned(cu_q, 4) || !aligned(ref, 4) || !aligned(step_len, 4))
+        return fail(DSPARK_EINVAL, "misaligned pointer");
+    dspark::PageBuffer to[kMaxBufs];
+    if (dspark_status st = check_page_bufs(bufs, n_bufs, to)) return st;
+    if (dspark_status st = check_page_ws(R, num_pages, ws, ws_bytes)) return st;
+    return hip_status(dspark::launch_pages_reserve(make_pages(block_table, max_pages, kv_len, R, page_size, ref, num_pages),
+                                                   cu_q, to, n_bufs, step_len, ws, (hipStream_t)stream),
+                      "dspark_pages_reserve");
+}
+
+dspark_status dspark_pages_commit(const int32_t* block_table, int max_pages, int32_t* kv_len, const int32_t* step_len,
+                                  const int32_t* cu_q, const int32_t* accepted_len, int R, int page_size, int32_t* ref,
+                                  int num_pages, dspark_stream stream) {
+    if (dspark_status st = check_page_sizes(R, max_pages, page_size, num_pages)) return st;
+    if (!block_table || !kv_len || !step_len || !cu_q || !ref) return fail(DSPARK_EINVAL, "null argument");
+    if (!aligned(block_table, 4) || !aligned(kv_len, 4) || !aligned(step_len, 4) || !aligned(cu_q, 4) ||
+        !aligned(accepted_len, 4) || !aligned(ref, 4))
+        return fail(DSPARK_EINVAL, "misaligned pointer");
+    return hip_status(dspark::launch_pages_drop(make_pages(block_table, max_pages, kv_len, R, page_size, ref, num_pages),
+                                                step_len, cu_q, accepted_len, nullptr, (hipStream_t)stream),
+                      "dspark_pages_commit");
+}
+
+dspark_status dspark_pages_trim(const int32_t* block_table, int max_pages, int32_t* kv_len, const int32_t* new_len, int R,
+                                int page_size, int32_t* ref, int num_pages, dspark_stream stream) {
+    if (dspark_status st = check_page_sizes(R, max_pages, page_size, num_pages)) return st;
+    if (!block_table || !kv_len || !new_len || !ref) return fail(DSPARK_EINVAL, "null argument");
+    if (!aligned(block_table, 4) || !aligned(kv_len, 4) || !aligned(new_len, 4) || !aligned(ref, 4))
+        return fail(DSPARK_EINVAL, "misaligned pointer");
+    return hip_status(dspark::launch_pages_drop(make_pages(block_table, max_pages, kv_len, R, page_size, ref, num_pages),
+                                                nullptr, nullptr, nullptr, new_len, (hipStream_t)stream),
+                      "dspark_pages_trim");
+}
+
+dspark_status dspark_pages_fork(int32_t* block_table, int max_pages, int32_t* kv_len, int R, int page_size, int32_t* ref,
+                                int num_pages, const int32_t* parent, const int32_t* child, const int32_t* len, int n,
+                                void* ws, size_t ws_bytes, dspark_stream stream) {
+    if (dspark_status st = check_page_sizes(R, max_pages, page_size, num_pages)) return st;
+    if (n < 0 || n > R) return fail(DSPARK_EINVAL, "n=%d outside [0, R=%d]", n, R);
+    if (!block_table || !kv_len || !ref || (n > 0 && (!parent || !child))) return fail(DSPARK_EINVAL, "null argument");
+    if (!aligned(block_table, 4) || !aligned(kv_len, 4) || !aligned(ref, 4) || !aligned(parent, 4) || !aligned(child, 4) ||
+        !aligned(len, 4))
+        return fail(DSPARK_EINVAL, "misaligned pointer");
+    if (dspark_status st = check_page_ws(R, num_pages, ws, ws_bytes)) return st;
+    if (n == 0) return ok();
+    return hip_status(dspark::launch_pages_fork(make_pages(block_table, max_pages, kv_len, R, page_size, ref, num_pages),
+                                                parent, child, len, n, ws, (hipStream_t)stream),
+                      "dspark_pages_fork");
+}
+
+dspark_status dspark_pages_compact(int32_t* block_table, int max_pages, const int32_t* kv_len, int R, int page_size,
+                                   int32_t* ref, int num_pages, const dspark_page_buffer* bufs, int n_bufs, int32_t* used,
+                                   void* ws, size_t ws_bytes, dspark_stream stream) {
+    if (dspark_status st = check_page_sizes(R, max_pages, page_size, num_pages)) return st;
+    if (!block_table || !kv_len || !ref || !used) return fail(DSPARK_EINVAL, "null argument");
+    if (!aligned(block_table, 4) || !aligned(kv_len, 4) || !aligned(ref, 4) || !aligned(used, 4))
+        return fail(DSPARK_EINVAL, "misaligned pointer");
+    dspark::PageBuffer to[kMaxBufs];
+    if (dspark_status st = check_page_bufs(bufs, n_bufs, to)) return st;
+    if (dspark_status st = check_page_ws(R, num_pages, ws, ws_bytes)) return st;
+    return hip_status(dspark::launch_pages_compact(make_pages(block_table, max_pages, kv_len, R, page_size, ref, num_pages),
+                                                   to, n_bufs, used, ws, (hipStream_t)stream),
+                      "dspark_pages_compact");
+}
+
+dspark_status dspark_check_page_inputs(const int32_t* block_table, int max_pages, const int32_t* kv_len, int R,
+                                       int page_size, const int32_t* ref, int num_pages, int32_t* report,
+                                       dspark_stream stream) {
+    if (dspark_status st = check_page_sizes(R, max_pages, page_size, num_pages)) return st;
+    if (!block_table || !kv_len || !ref || !report) return fail(DSPARK_EINVAL, "null argument");
+    if (!aligned(block_table, 4) || !aligned(kv_len, 4) || !aligned(ref, 4) || !aligned(report, 4))
+        return fail(DSPARK_EINVAL, "misaligned pointer");
+    return hip_status(dspark::launch_check_pages(block_table, max_pages, kv_len, R, page_size, ref, num_pages, report,
+                                                 (hipStream_t)stream),
+                      "dspark_check_page_inputs");
 }
 
 // ------------------------------------------------------------------ acceptance

@@ -53,6 +53,59 @@ hipError_t launch_attn_stream(const AttnArgs& a, void* ws, hipStream_t s);
 size_t attn_generic_workspace(const AttnArgs& a);
 hipError_t launch_attn_generic(const AttnArgs& a, void* ws, hipStream_t s);
 
+// ---- the cache in 8 bits: e4m3 codes, a scale for each block of tokens and head ------
+struct CacheScales {
+    const float* k;  // [num_pages, Hkv, page / block]
+    const float* v;
+    int block;       // tokens of a scale
+    int num_pages;   // table entries outside [0, num_pages) read the nearest page inside
+};
+// (k, v and their strides of `a` are in codes)
+hipError_t launch_attn_generic_scaled(const AttnArgs& a, const CacheScales& c, void* ws, hipStream_t s);
+
+struct AppendArgs {
+    const void* k;  // new rows [total_q, Hkv, D], a row every k_ld elements
+    const void* v;  // null: the cache has keys alone
+    int64_t k_ld, v_ld;
+    int bf16;
+    void* k_cache;
+    void* v_cache;
+    int64_t ks[3], vs[3];
+    float* k_scale;
+    float* v_scale;
+    int block;
+    const int32_t* block_table;
+    int max_pages, num_pages;
+    const int32_t* kv_len;
+    const int32_t* cu_q;
+    int R, max_q, Hkv, Dqk, Dv, page;
+};
+hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
+
+// ---- the pages of a cache ---------------------------------------------------------
+struct PageArgs {
+    int32_t* block_table;
+    int max_pages;
+    int32_t* kv_len;
+    int R, page;
+    int32_t* ref;  // [num_pages] entries that name the page
+    int num_pages;
+};
+struct PageBuffer {
+    void* base;
+    int64_t stride, bytes;
+};
+size_t pages_workspace(int R, int num_pages);
+hipError_t launch_pages_fork(const PageArgs& a, const int32_t* parent, const int32_t* child, const int32_t* len, int n,
+                             void* ws, hipStream_t s);
+hipError_t launch_pages_reserve(const PageArgs& a, const int32_t* cu_q, const PageBuffer* bufs, int n_bufs,
+                                int32_t* step_len, void* ws, hipStream_t s);
+// the step's tokens kept: 1 + accepted (accepted null: all); with cu_q null, min(kv_len, new_len)
+hipError_t launch_pages_drop(const PageArgs& a, const int32_t* step_len, const int32_t* cu_q, const int32_t* accepted,
+                             const int32_t* new_len, hipStream_t s);
+hipError_t launch_pages_compact(const PageArgs& a, const PageBuffer* bufs, int n_bufs, int32_t* used, void* ws,
+                                hipStream_t s);
+
 // ---- acceptance ------------------------------------------------------------------
 struct AcceptArgs {
     const int32_t* draft_tok;
@@ -105,6 +158,8 @@ hipError_t launch_markov(const MarkovArgs& a, void* ws, hipStream_t s);
 hipError_t launch_check_verify(const int32_t* block_table, int max_pages, const int32_t* kv_len,
                                const int32_t* cu_q, int R, int max_q, int page_size, int num_pages,
                                int32_t* report, hipStream_t s);
+hipError_t launch_check_pages(const int32_t* block_table, int max_pages, const int32_t* kv_len, int R, int page_size,
+                              const int32_t* ref, int num_pages, int32_t* report, hipStream_t s);
 hipError_t launch_check_accept(const int32_t* cu_q, const float* u, int R, int K, int32_t* report,
                                hipStream_t s);
 hipError_t launch_check_schedule(const float* conf, int R, int K, int32_t* report, hipStream_t s);

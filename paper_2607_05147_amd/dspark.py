@@ -87,6 +87,28 @@ def lib():
         L.dspark_check_schedule_inputs.argtypes = [p, i32, i32, p, p]
         L.dspark_check_draft_inputs.restype = i32
         L.dspark_check_draft_inputs.argtypes = [p, p, i32, i32, p, p]
+        L.dspark_cache_append.restype = i32
+        L.dspark_cache_append.argtypes = [p, p, i64, i64, i32, p, p, p, p, p, p, i32, p, i32, i32, p, p,
+                                          i32, i32, i32, i32, i32, i32, p]
+        L.dspark_verify_attn_scaled_workspace_size.restype = sz
+        L.dspark_verify_attn_scaled_workspace_size.argtypes = [i32] * 10
+        L.dspark_verify_attn_scaled.restype = i32
+        L.dspark_verify_attn_scaled.argtypes = [p, p, p, p, p, p, p, i32, p, i32, i32, p, p, i32, i32, i32,
+                                                i32, i32, i32, i32, f32, i32, p, p, p, sz, p]
+        L.dspark_pages_workspace_size.restype = sz
+        L.dspark_pages_workspace_size.argtypes = [i32, i32]
+        L.dspark_pages_reserve.restype = i32
+        L.dspark_pages_reserve.argtypes = [p, i32, p, p, i32, i32, p, i32, p, i32, p, p, sz, p]
+        L.dspark_pages_commit.restype = i32
+        L.dspark_pages_commit.argtypes = [p, i32, p, p, p, p, i32, i32, p, i32, p]
+        L.dspark_pages_trim.restype = i32
+        L.dspark_pages_trim.argtypes = [p, i32, p, p, i32, i32, p, i32, p]
+        L.dspark_pages_fork.restype = i32
+        L.dspark_pages_fork.argtypes = [p, i32, p, i32, i32, p, i32, p, p, p, i32, p, sz, p]
+        L.dspark_pages_compact.restype = i32
+        L.dspark_pages_compact.argtypes = [p, i32, p, i32, i32, p, i32, p, i32, p, p, sz, p]
+        L.dspark_check_page_inputs.restype = i32
+        L.dspark_check_page_inputs.argtypes = [p, i32, p, i32, i32, p, i32, p, p]
         _lib = L
     return _lib
 
@@ -156,6 +178,8 @@ CHECK_RULES = {
                3: "uniform outside [0, 1)"},
     "schedule": {1: "confidence outside [0, 1]"},
     "draft": {1: "temperature not finite and positive", 2: "uniform outside [0, 1)"},
+    "pages": {1: "kv_len outside [0, max_pages * page_size]", 2: "held table entry outside the cache",
+              3: "held table entry names a page without holders"},
 }
 
 
@@ -218,6 +242,18 @@ def check_draft_inputs(u: torch.Tensor, sts_temp: Optional[torch.Tensor] = None,
     st = lib().dspark_check_draft_inputs(_p(u), _p(sts_temp), R, K, _p(report), _stream(stream))
     _raise(st, "dspark_check_draft_inputs")
     return _report(report, "draft", stream)
+
+
+def check_page_inputs(block_table: torch.Tensor, kv_len: torch.Tensor, page_size: int, ref: torch.Tensor,
+                      stream=None) -> Optional[tuple]:
+    """First broken rule of the dspark_pages_* state as (code, request, index,
+    value, rule) or None; waits for the check."""
+    R, max_pages, num_pages = _page_state(block_table, kv_len, ref)
+    report = torch.empty(4, dtype=torch.int32, device=ref.device)
+    st = lib().dspark_check_page_inputs(_p(block_table), max_pages, _p(kv_len), R, page_size, _p(ref), num_pages,
+                                        _p(report), _stream(stream))
+    _raise(st, "dspark_check_page_inputs")
+    return _report(report, "pages", stream)
 
 
 def _cache_pages(cache: torch.Tensor, strides: Sequence[int], heads: int, page_size: int, dim: int) -> int:
@@ -383,6 +419,293 @@ def dspark_verify_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
                                   ws_bytes, _stream(stream))
     _raise(st, "dspark_verify_attn")
     return out, lse
+
+
+# ------------------------------------------------------------------ the cache in 8 bits
+
+_CODES = (torch.uint8, torch.float8_e4m3fn)
+
+
+def _on(stream, *tensors) -> C.c_void_p:
+    """The stream's handle; every tensor has to be on its device, the current one."""
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    for t in tensors:
+        if t is not None and t.device != stream.device:
+            raise DSparkError(f"a tensor on {t.device}, the call's stream on {stream.device}")
+    if stream.device.index != torch.cuda.current_device():
+        raise DSparkError(f"the call's stream is on {stream.device}, the current device is {torch.cuda.current_device()}")
+    return C.c_void_p(stream.cuda_stream)
+
+
+def _used_on(stream, *tensors) -> None:
+    """Tensors that a call allocated itself, where it runs on another stream than the current one."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _scaled_cache(k_cache, v_cache, k_strides, v_strides, k_scale, v_scale, block, block_table, kv_len, cu_q, page_size,
+                  Dqk, Dv):
+    """Checks of a cache of e4m3 codes; returns (R, max_pages, num_pages, Hkv)."""
+    if block < 1 or page_size < 1 or page_size % block:
+        raise DSparkError(f"block={block} must divide page_size={page_size}")
+    _dev(k_scale, "k_scale", torch.float32)
+    if k_scale.dim() != 3 or k_scale.shape[2] != page_size // block:
+        raise DSparkError("k_scale must be [num_pages, Hkv, page_size / block]")
+    num_pages, Hkv = k_scale.shape[:2]
+    for t, st, sc, D, name in ((k_cache, k_strides, k_scale, Dqk, "k"), (v_cache, v_strides, v_scale, Dv, "v")):
+        if t is None:
+            continue
+        _dev(t, name + "_cache")
+        if t.dtype not in _CODES:
+            raise DSparkError(f"{name}_cache must be uint8 or float8_e4m3fn, got {t.dtype}")
+        _dev(sc, name + "_scale", torch.float32, k_scale.shape)
+        if _cache_pages(t, st, Hkv, page_size, D) < num_pages:
+            raise DSparkError(f"{name}_cache holds fewer than {num_pages} pages of these strides")
+    _dev(block_table, "block_table", torch.int32)
+    if block_table.dim() != 2:
+        raise DSparkError("block_table must be [R, max_pages]")
+    R, max_pages = block_table.shape
+    _dev(kv_len, "kv_len", torch.int32, (R,))
+    _dev(cu_q, "cu_q", torch.int32, (R + 1,))
+    return R, max_pages, num_pages, Hkv
+
+
+def _strides3(st):
+    return (C.c_int64 * 3)(*[int(x) for x in st])
+
+
+def _new_rows(t, name, dtype, Hkv):
+    """[rows, Hkv, D] whose rows may lie apart: (D, row stride)."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.dim() != 3 or t.dtype != dtype:
+        raise DSparkError(f"{name} must be a [rows, Hkv, D] {dtype} ROCm tensor")
+    D = t.shape[2]
+    if t.shape[1] != Hkv or (D > 1 and t.stride(2) != 1) or (Hkv > 1 and t.stride(1) != D):
+        raise DSparkError(f"{name} must have Hkv={Hkv} heads, dense within a row")
+    return D, t.stride(0) if t.shape[0] > 1 else max(t.stride(0), Hkv * D)
+
+
+def dspark_cache_append(k: torch.Tensor, v: Optional[torch.Tensor], k_cache: torch.Tensor,
+                        v_cache: Optional[torch.Tensor], k_strides: Sequence[int],
+                        v_strides: Optional[Sequence[int]], k_scale: torch.Tensor,
+                        v_scale: Optional[torch.Tensor], block: int, block_table: torch.Tensor,
+                        kv_len: torch.Tensor, cu_q: torch.Tensor, max_q: int, page_size: int, stream=None) -> None:
+    """k [rows, Hkv, Dqk], v [rows, Hkv, Dv] (fp32/bf16, rows may be a part of wider ones) ->
+    codes in k_cache, v_cache (uint8 or float8_e4m3fn, flat or shaped, addressed by strides in bytes)
+    and fp32 k_scale, v_scale [num_pages, Hkv, page_size / block], in place.  v, v_cache and v_scale
+    None: keys alone."""
+    if not isinstance(k, torch.Tensor) or k.dtype not in _DT:
+        raise DSparkError("k must be float32 or bfloat16")
+    if (v is None) != (v_cache is None) or (v is None) != (v_scale is None) or (v is not None and v_strides is None):
+        raise DSparkError("v, v_cache, v_strides and v_scale go together")
+    Hkv = k.shape[1] if k.dim() == 3 else 0
+    Dqk, k_ld = _new_rows(k, "k", k.dtype, Hkv)
+    Dv, v_ld = (0, 0) if v is None else _new_rows(v, "v", k.dtype, Hkv)
+    if v is not None and v.shape[0] != k.shape[0]:
+        raise DSparkError("k and v must have the same rows")
+    R, max_pages, num_pages, heads = _scaled_cache(k_cache, v_cache, k_strides, v_strides, k_scale, v_scale, block,
+                                                   block_table, kv_len, cu_q, page_size, Dqk, Dv)
+    if heads != Hkv:
+        raise DSparkError(f"k has {Hkv} heads, k_scale {heads}")
+    on = _on(stream, k, v, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, cu_q)
+    if debug_checks():
+        _debug_raise(check_verify_inputs(block_table, kv_len, cu_q, max_q, page_size, num_pages, stream),
+                     "dspark_cache_append")
+    st = lib().dspark_cache_append(C.c_void_p(k.data_ptr()), None if v is None else C.c_void_p(v.data_ptr()), k_ld, v_ld,
+                                   _DT[k.dtype], _p(k_cache), _p(v_cache), _strides3(k_strides),
+                                   None if v is None else _strides3(v_strides), _p(k_scale), _p(v_scale), block,
+                                   _p(block_table), max_pages, num_pages, _p(kv_len), _p(cu_q), R, max_q, Hkv, Dqk, Dv,
+                                   page_size, on)
+    _raise(st, "dspark_cache_append")
+
+
+def dspark_verify_attn_scaled_workspace_size(R: int, max_q: int, Hq: int, Hkv: int, Dqk: int, Dv: int, max_pages: int,
+                                             page_size: int, block: int, dtype: torch.dtype) -> int:
+    return int(lib().dspark_verify_attn_scaled_workspace_size(R, max_q, Hq, Hkv, Dqk, Dv, max_pages, page_size, block,
+                                                              _DT[dtype]))
+
+
+def dspark_verify_attn_scaled(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                              k_strides: Sequence[int], v_strides: Sequence[int], k_scale: torch.Tensor,
+                              v_scale: torch.Tensor, block: int, block_table: torch.Tensor, kv_len: torch.Tensor,
+                              cu_q: torch.Tensor, max_q: int, Dv: int, page_size: int, scale: float,
+                              out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                              want_lse: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
+    """dspark_verify_attn over a cache of e4m3 codes and scales (dspark_cache_append's).
+    q [total_q(or more rows), Hq, Dqk]; returns (out [rows of q, Hq, Dv], lse|None)."""
+    _dev(q, "q")
+    if q.dtype not in _DT or q.dim() != 3:
+        raise DSparkError("q must be a float32 or bfloat16 [tokens, Hq, Dqk] tensor")
+    rows, Hq, Dqk = q.shape
+    R, max_pages, num_pages, Hkv = _scaled_cache(k_cache, v_cache, k_strides, v_strides, k_scale, v_scale, block,
+                                                 block_table, kv_len, cu_q, page_size, Dqk, Dv)
+    if out is None:
+        out = torch.empty((rows, Hq, Dv), dtype=q.dtype, device=q.device)
+        _used_on(stream, out)
+    _dev(out, "out", q.dtype, (rows, Hq, Dv))
+    if lse is None and want_lse:
+        lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
+        _used_on(stream, lse)
+    _dev(lse, "lse", torch.float32, (rows, Hq), optional=True)
+    if ws is None:
+        need = dspark_verify_attn_scaled_workspace_size(R, max_q, Hq, Hkv, Dqk, Dv, max_pages, page_size, block, q.dtype)
+        ws, ws_bytes = _workspace(need, q.device, None)
+        _used_on(stream, ws)
+    else:
+        ws_bytes = ws.numel() * ws.element_size()
+    on = _on(stream, q, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, cu_q, out, lse, ws)
+    if debug_checks():
+        _debug_raise(check_verify_inputs(block_table, kv_len, cu_q, max_q, page_size, num_pages, stream),
+                     "dspark_verify_attn_scaled")
+    st = lib().dspark_verify_attn_scaled(_p(q), _p(k_cache), _p(v_cache), _strides3(k_strides), _strides3(v_strides),
+                                         _p(k_scale), _p(v_scale), block, _p(block_table), max_pages, num_pages,
+                                         _p(kv_len), _p(cu_q), R, max_q, Hq, Hkv, Dqk, Dv, page_size, float(scale),
+                                         _DT[q.dtype], _p(out), _p(lse), _p(ws), ws_bytes, on)
+    _raise(st, "dspark_verify_attn_scaled")
+    return out, lse
+
+
+# ------------------------------------------------------------------ the pages of a cache
+
+class _PageBuffer(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("page_stride", C.c_int64), ("page_bytes", C.c_int64)]
+
+
+class PageBuffers:
+    """The memory that a cache's pages are made of: contiguous tensors of num_pages equal parts
+    (keys, values and scales, layer by layer).  Keeps the tensors alive; made once for a cache."""
+
+    def __init__(self, tensors: Sequence[torch.Tensor], num_pages: int):
+        self.tensors, self.num_pages = list(tensors), num_pages
+        self.array = (_PageBuffer * max(1, len(self.tensors)))()
+        for i, t in enumerate(self.tensors):
+            _dev(t, f"buffer {i}")
+            if t.device != self.tensors[0].device:
+                raise DSparkError("the buffers of a cache are on one device")
+            n = t.numel() * t.element_size()
+            if num_pages < 1 or n == 0 or n % num_pages:
+                raise DSparkError(f"buffer {i}: {n} bytes are not {num_pages} pages")
+            self.array[i] = _PageBuffer(t.data_ptr(), n // num_pages, n // num_pages)
+
+
+def page_buffers(tensors: Sequence[torch.Tensor], num_pages: int) -> PageBuffers:
+    return PageBuffers(tensors, num_pages)
+
+
+def dspark_pages_workspace_size(R: int, num_pages: int) -> int:
+    return int(lib().dspark_pages_workspace_size(R, num_pages))
+
+
+def _page_state(block_table, kv_len, ref):
+    _dev(block_table, "block_table", torch.int32)
+    if block_table.dim() != 2:
+        raise DSparkError("block_table must be [R, max_pages]")
+    R, max_pages = block_table.shape
+    _dev(kv_len, "kv_len", torch.int32, (R,))
+    _dev(ref, "ref", torch.int32)
+    if ref.dim() != 1:
+        raise DSparkError("ref must be [num_pages]")
+    return R, max_pages, ref.shape[0]
+
+
+def _page_call(block_table, kv_len, page_size, ref, bufs, ws, what, stream):
+    """What reserve, fork and compact share: sizes, buffers, workspace and the state's check."""
+    R, max_pages, num_pages = _page_state(block_table, kv_len, ref)
+    if bufs is not None and bufs.num_pages != num_pages:
+        raise DSparkError(f"bufs hold {bufs.num_pages} pages, ref {num_pages}")
+    if ws is None:
+        ws, ws_bytes = _workspace(dspark_pages_workspace_size(R, num_pages), ref.device, None)
+        _used_on(stream, ws)
+    else:
+        ws_bytes = ws.numel() * ws.element_size()
+    _on(stream, block_table, kv_len, ref, ws, *([] if bufs is None else bufs.tensors[:1]))
+    if debug_checks():
+        _debug_raise(check_page_inputs(block_table, kv_len, page_size, ref, stream), what)
+    return R, max_pages, num_pages, ws, ws_bytes
+
+
+def dspark_pages_reserve(block_table: torch.Tensor, kv_len: torch.Tensor, cu_q: torch.Tensor, page_size: int,
+                         ref: torch.Tensor, bufs: Optional[PageBuffers] = None, step_len: Optional[torch.Tensor] = None,
+                         ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Pages for cu_q[r+1] - cu_q[r] more tokens of each request; block_table and ref change in place.
+    Returns step_len int32 [R], the kv_len of the step (0: not served).  bufs: what is copied where a
+    partly filled page is shared (None: nothing)."""
+    R, max_pages, num_pages, ws, ws_bytes = _page_call(block_table, kv_len, page_size, ref, bufs, ws,
+                                                       "dspark_pages_reserve", stream)
+    _dev(cu_q, "cu_q", torch.int32, (R + 1,))
+    if step_len is None:
+        step_len = torch.empty(R, dtype=torch.int32, device=ref.device)
+        _used_on(stream, step_len)
+    _dev(step_len, "step_len", torch.int32, (R,))
+    st = lib().dspark_pages_reserve(_p(block_table), max_pages, _p(kv_len), _p(cu_q), R, page_size, _p(ref), num_pages,
+                                    None if bufs is None else bufs.array, 0 if bufs is None else len(bufs.tensors),
+                                    _p(step_len), _p(ws), ws_bytes, _on(stream, cu_q, step_len))
+    _raise(st, "dspark_pages_reserve")
+    return step_len
+
+
+def dspark_pages_commit(block_table: torch.Tensor, kv_len: torch.Tensor, step_len: torch.Tensor, cu_q: torch.Tensor,
+                        page_size: int, ref: torch.Tensor, accepted_len: Optional[torch.Tensor] = None,
+                        stream=None) -> None:
+    """After a step: each request keeps 1 + accepted_len of its tokens (None: all); kv_len and ref change in place."""
+    R, max_pages, num_pages = _page_state(block_table, kv_len, ref)
+    _dev(step_len, "step_len", torch.int32, (R,))
+    _dev(cu_q, "cu_q", torch.int32, (R + 1,))
+    _dev(accepted_len, "accepted_len", torch.int32, (R,), optional=True)
+    st = lib().dspark_pages_commit(_p(block_table), max_pages, _p(kv_len), _p(step_len), _p(cu_q), _p(accepted_len), R,
+                                   page_size, _p(ref), num_pages,
+                                   _on(stream, block_table, kv_len, step_len, cu_q, accepted_len, ref))
+    _raise(st, "dspark_pages_commit")
+
+
+def dspark_pages_trim(block_table: torch.Tensor, kv_len: torch.Tensor, new_len: torch.Tensor, page_size: int,
+                      ref: torch.Tensor, stream=None) -> None:
+    """kv_len = min(kv_len, new_len) (0: the request ends); kv_len and ref change in place."""
+    R, max_pages, num_pages = _page_state(block_table, kv_len, ref)
+    _dev(new_len, "new_len", torch.int32, (R,))
+    on = _on(stream, block_table, kv_len, new_len, ref)
+    if debug_checks():
+        _debug_raise(check_page_inputs(block_table, kv_len, page_size, ref, stream), "dspark_pages_trim")
+    st = lib().dspark_pages_trim(_p(block_table), max_pages, _p(kv_len), _p(new_len), R, page_size, _p(ref), num_pages,
+                                 on)
+    _raise(st, "dspark_pages_trim")
+
+
+def dspark_pages_fork(block_table: torch.Tensor, kv_len: torch.Tensor, page_size: int, ref: torch.Tensor,
+                      parent: torch.Tensor, child: torch.Tensor, len: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Requests child [n] (of length 0) share the pages of parent [n], up to len [n] tokens (None: all);
+    block_table, kv_len and ref change in place."""
+    R, max_pages, num_pages, ws, ws_bytes = _page_call(block_table, kv_len, page_size, ref, None, ws, "dspark_pages_fork",
+                                                       stream)
+    _dev(parent, "parent", torch.int32)
+    n = parent.numel()
+    _dev(parent, "parent", torch.int32, (n,))
+    _dev(child, "child", torch.int32, (n,))
+    _dev(len, "len", torch.int32, (n,), optional=True)
+    st = lib().dspark_pages_fork(_p(block_table), max_pages, _p(kv_len), R, page_size, _p(ref), num_pages, _p(parent),
+                                 _p(child), _p(len), n, _p(ws), ws_bytes, _on(stream, parent, child, len))
+    _raise(st, "dspark_pages_fork")
+
+
+def dspark_pages_compact(block_table: torch.Tensor, kv_len: torch.Tensor, page_size: int, ref: torch.Tensor,
+                         bufs: Optional[PageBuffers] = None, used: Optional[torch.Tensor] = None,
+                         ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Moves the pages in use to ids 0 .. used - 1; block_table, ref and the buffers change in place.
+    Returns used int32 [1] (device)."""
+    R, max_pages, num_pages, ws, ws_bytes = _page_call(block_table, kv_len, page_size, ref, bufs, ws,
+                                                       "dspark_pages_compact", stream)
+    if used is None:
+        used = torch.empty(1, dtype=torch.int32, device=ref.device)
+        _used_on(stream, used)
+    _dev(used, "used", torch.int32, (1,))
+    st = lib().dspark_pages_compact(_p(block_table), max_pages, _p(kv_len), R, page_size, _p(ref), num_pages,
+                                    None if bufs is None else bufs.array, 0 if bufs is None else len(bufs.tensors),
+                                    _p(used), _p(ws), ws_bytes, _on(stream, used))
+    _raise(st, "dspark_pages_compact")
+    return used
 
 
 # ------------------------------------------------------------------ stage 3
