@@ -269,7 +269,14 @@ dspark_status dspark_verify_attn(const void* q, const void* k_cache, const void*
  * dspark_verify_attn_scaled is dspark_verify_attn over such a cache: the same
  * arguments, rules, outputs and limits (dt: queries and output; the softmax in
  * fp32).  Table entries outside [0, num_pages) read the nearest page inside.
- * v_cache may alias k_cache, with v_scale = k_scale.
+ * v_cache may alias k_cache, with v_scale = k_scale.  Which kernels run:
+ *   - head sizes up to 256, cache strides multiples of 16 bytes (page stride
+ *     below 2^31, token stride below 2^24), q, k_cache and v_cache 16-byte and
+ *     out 8-byte (bf16) or 16-byte (fp32) aligned, Dqk and Dv multiples of 16:
+ *     matrix cores, the codes widened to bf16 (exact), bf16 queries as they are,
+ *     fp32 queries as three bf16 terms (exact), probabilities as two (bf16) or
+ *     three (fp32) bf16 terms; HBM-bound;
+ *   - anything else: vector ALUs.
  *   ws of dspark_verify_attn_scaled_workspace_size bytes, 256-aligned; a smaller
  *   one is refused (DSPARK_EWORKSPACE).  A non-finite key, value or scale
  *   reaches only the rows that see it.

@@ -98,6 +98,18 @@ __device__ __forceinline__ void lds_copy16(const void* gsrc, uint32_t lds_addr) 
         : "memory", "m0");
 }
 
+// 4-byte copy: lane L's 4 bytes land at lds_addr + 4 L.
+__device__ __forceinline__ void lds_copy4(const void* gsrc, uint32_t lds_addr) {
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane(lds_addr);
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dword %1, off"
+        :
+        : "s"(m0), "v"(gsrc)
+        : "memory", "m0");
+}
+
 // a wave-uniform 64-bit value, in scalar registers
 __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);

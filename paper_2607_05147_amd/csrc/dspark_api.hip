@@ -422,7 +422,8 @@ size_t dspark_verify_attn_scaled_workspace_size(int R, int max_q, int Hq, int Hk
         return 0;
     dspark::AttnArgs a = make_attn(nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, max_pages, nullptr, nullptr, R,
                                    max_q, Hq, Hkv, Dqk, Dv, page_size, 1.0f, dt, nullptr, nullptr);
-    return dspark::attn_generic_workspace(a);
+    const size_t need = dspark::attn_generic_workspace(a);
+    return dspark::attn_scaled_shape_ok(a) ? std::max(need, dspark::attn_scaled_workspace(a)) : need;
 }
 
 dspark_status dspark_verify_attn_scaled(const void* q, const void* k_cache, const void* v_cache,
@@ -448,10 +449,14 @@ dspark_status dspark_verify_attn_scaled(const void* q, const void* k_cache, cons
     const dspark::AttnArgs a = make_attn(q, k_cache, v_cache, k_strides, v_strides, block_table, max_pages, kv_len, cu_q,
                                          R, max_q, Hq, Hkv, Dqk, Dv, page_size, scale, dt, out, lse);
     const dspark::CacheScales c = {k_scale, v_scale, block, num_pages};
-    const size_t need = dspark::attn_generic_workspace(a);
+    // (a call is refused alike whatever its strides and alignment, which decide the kernels)
+    size_t need = dspark::attn_generic_workspace(a);
+    if (dspark::attn_scaled_shape_ok(a)) need = std::max(need, dspark::attn_scaled_workspace(a));
     if (ws_bytes < need || (need > 0 && !ws) || !aligned(ws, 256))
         return fail(DSPARK_EWORKSPACE, "workspace of %zu bytes (256-aligned) needed, got %zu", need, ws_bytes);
-    return hip_status(dspark::launch_attn_generic_scaled(a, c, ws, (hipStream_t)stream), "dspark_verify_attn_scaled");
+    return hip_status(dspark::attn_scaled_supported(a, c) ? dspark::launch_attn_scaled(a, c, ws, (hipStream_t)stream)
+                                                          : dspark::launch_attn_generic_scaled(a, c, ws, (hipStream_t)stream),
+                      "dspark_verify_attn_scaled");
 }
 
 // ------------------------------------------------------------------ pages

@@ -61,6 +61,10 @@ struct CacheScales {
     int num_pages;   // table entries outside [0, num_pages) read the nearest page inside
 };
 // (k, v and their strides of `a` are in codes)
+bool attn_scaled_shape_ok(const AttnArgs& a);                          // shape only (workspace sizing)
+bool attn_scaled_supported(const AttnArgs& a, const CacheScales& c);  // shape and alignment
+size_t attn_scaled_workspace(const AttnArgs& a);
+hipError_t launch_attn_scaled(const AttnArgs& a, const CacheScales& c, void* ws, hipStream_t s);
 hipError_t launch_attn_generic_scaled(const AttnArgs& a, const CacheScales& c, void* ws, hipStream_t s);
 
 struct AppendArgs {
