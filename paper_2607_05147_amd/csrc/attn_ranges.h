@@ -110,7 +110,12 @@ __device__ __forceinline__ bool range_find(const Ranges& p, int w, int total_row
 // this worker's range, in order: steps [s0, s1) of the chunk's ns; the partial,
 // when they are not all, goes to `slot` (0: it starts inside the chunk, so it
 // is the worker's first; 1: it ends inside, its last).
-template <int STEP, typename F>
+//
+// XCD (with by_head; a grid of a multiple of 8 * Hkv): the heads of a range go to one XCD,
+// block b to XCD b % 8 as the device deals them, so that what the heads share of a page's
+// lines is fetched into one L2.
+constexpr int kXcds = 8;
+template <int STEP, bool XCD = false, typename F>
 __device__ __forceinline__ void range_walk(const Ranges& p, F f) {
     const AttnArgs& a = p.a;
     const int total_rows = range_total_rows(a);
@@ -123,9 +128,14 @@ __device__ __forceinline__ void range_walk(const Ranges& p, F f) {
         return;
     }
     const int heads = p.by_head ? 1 : a.Hkv;  // of this worker's list
+    int worker = blockIdx.x;
+    if (XCD && p.by_head) {
+        const int i = blockIdx.x / kXcds;
+        worker = (i / a.Hkv * kXcds + blockIdx.x % kXcds) * a.Hkv + i % a.Hkv;
+    }
     int64_t u0, u1, ur;
     int r;
-    if (!range_find<STEP>(p, p.by_head ? blockIdx.x / a.Hkv : blockIdx.x, total_rows, u0, u1, r, ur)) return;
+    if (!range_find<STEP>(p, p.by_head ? worker / a.Hkv : worker, total_rows, u0, u1, r, ur)) return;
     int64_t u = u0;
     while (u < u1) {  // (r stays below R: the requests from r on hold the units up to u1)
         int q0, ql, kv;
@@ -139,12 +149,12 @@ __device__ __forceinline__ void range_walk(const Ranges& p, F f) {
             const int item = local / ns;
             const int s0 = local - item * ns;
             const int gl = item / nrc;
-            const int g = p.by_head ? (int)(blockIdx.x % a.Hkv) : gl;
+            const int g = p.by_head ? worker % a.Hkv : gl;
             const int s1 = (int)min((int64_t)ns, s0 + (u1 - u));
             f(r, __builtin_amdgcn_readfirstlane(g), __builtin_amdgcn_readfirstlane(item - gl * nrc), __builtin_amdgcn_readfirstlane(q0),
               __builtin_amdgcn_readfirstlane(ql), __builtin_amdgcn_readfirstlane(kv),
               __builtin_amdgcn_readfirstlane(s0), __builtin_amdgcn_readfirstlane(s1), __builtin_amdgcn_readfirstlane(ns),
-              2 * (int64_t)blockIdx.x + (s0 == 0));
+              2 * (int64_t)worker + (s0 == 0));
             local += s1 - s0;
             u += s1 - s0;
         }

@@ -39,7 +39,9 @@
 namespace dspark {
 namespace scaled {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -50,15 +52,21 @@ typedef __attribute__((address_space(3))) float lds_f32;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kRescale = 8.0f;     // log2 headroom before the running max is moved
+// The running reference of a row's scores moves when one exceeds it by 2^kHead, to kBias
+// below that.  fp32: p is at most 2^8.  bf16 queries, p in fp16: at most 2^15, and full
+// precision down to 2^-21 of the row's largest (fp16 is normal from 2^-14).
+template <bool F32> struct Ref {
+    static constexpr float kBias = F32 ? 0.0f : 7.0f, kHead = F32 ? 8.0f : 15.0f;
+};
 constexpr int kMinUnits = 4;         // steps per wave, at least
 constexpr int kPageRegs = 2;         // page ids per lane: 128 pages of a range at a time
 constexpr int kMaxD = 256;
 
-// CH: 16-byte chunks of an LDS row: head sizes up to 16 * CH.  NT: 16-row tiles.
-template <bool F32, int CH, int NT>
+// CH: 16-byte chunks of an LDS row: head sizes up to 16 * CH.  W: waves of a worker;
+// T: 16-row tiles of a wave.
+template <bool F32, int CH, int W, int T>
 struct Cfg {
-    static constexpr int H = CH <= 8 ? 2 : 1;   // 32-key halves of a step
+    static constexpr int H = CH <= (W == 1 ? 4 : 8) ? 2 : 1;  // 32-key halves of a step
     static constexpr int Step = 32 * H;
     static constexpr int P = 2 * H;             // 16-key pieces
     static constexpr int S = CH / 4;            // 16-byte operand reads of a key; copies of a piece
@@ -66,13 +74,20 @@ struct Cfg {
     static constexpr int TileB = Step * RowB;
     static constexpr int Dp = 16 * CH;          // padded head size
     static constexpr int DB = CH;               // 16-dim output blocks
-    static constexpr int TQ = F32 ? 3 : 1, TP = F32 ? 3 : 2;  // bf16 terms of a query, a probability
-    static constexpr int LdsB = 2 * TileB + 256;              // K, V, scales
-    static constexpr int LdsWaves = 160 * 1024 / LdsB;
+    static constexpr int TQ = F32 ? 3 : 1;      // terms of a query (bf16)
+    static constexpr int TP = F32 ? 3 : 1;      // of a probability (bf16; fp16)
+    static constexpr int Rows = 16 * W * T;     // of a chunk
+    // scales in LDS: of piece h at h * ScaleStep, the values' ScaleV behind the keys'
+    static constexpr int ScaleStep = W == 1 ? 4 : 256 * W / P, ScaleV = W == 1 ? 4 * P : 4;
+    static constexpr int BufB = 2 * TileB + 256 * W;          // K, V, scales
+    static constexpr int Ring = W == 1 ? 1 : 3;  // buffers
+    static constexpr int LdsB = Ring * BufB;
+    static constexpr int LdsFit = 160 * 1024 / LdsB;          // workers of a CU, by LDS
     // registers: accumulators, queries, scores and probabilities of the row tiles; operands
-    static constexpr int Regs = NT * (4 * DB + 8 * S * TQ + 8 * H * (TP > 2 ? TP + 1 : 2)) + 8 * H * S + 56;
-    static constexpr int Eu = Regs <= 128 && LdsWaves >= 16 ? 4 : Regs <= 168 && LdsWaves >= 12 ? 3 : Regs <= 256 && LdsWaves >= 8 ? 2 : 1;
-    static constexpr int Cu = LdsWaves < 4 * Eu ? LdsWaves : 4 * Eu;  // waves per CU
+    static constexpr int Regs = T * (4 * DB + 8 * S * TQ + 8 * (W == 1 ? H : 1) * (TP > 2 ? TP + 1 : 2)) + 8 * (W == 1 ? H : 1) * S + 84;
+    static constexpr int RegFit = (Regs <= 128 ? 16 : Regs <= 168 ? 12 : Regs <= 256 ? 8 : 4) / W;
+    static constexpr int Cu = LdsFit < RegFit ? LdsFit : RegFit;  // workers of a CU
+    static constexpr int Eu = Cu * W >= 16 ? 4 : Cu * W >= 12 ? 3 : Cu * W >= 8 ? 2 : 1;  // waves of a SIMD
 };
 
 struct Params : Ranges {
@@ -81,6 +96,7 @@ struct Params : Ranges {
     uint32_t ks0, vs0, ks2, vs2;
     int pad;                         // some row is shorter than the LDS row
     int nb;                          // blocks of a page
+    uint32_t per_block;              // ceil(2^32 / (16-key pieces of a block))
     float scale2;
 };
 
@@ -119,7 +135,17 @@ __device__ __forceinline__ void wait_copies() {
 
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// eight codes as bf16
+// eight codes as fp16 (exact)
+__device__ __forceinline__ f16x8 widen_half(uint32_t lo, uint32_t hi) {
+    u32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+    return __builtin_bit_cast(f16x8, r);
+}
+
+// eight codes as bf16 (exact)
 __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
     u32x4 r;
     r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
@@ -142,32 +168,53 @@ __device__ __forceinline__ void terms(float a, float b, uint32_t (&w)[T]) {
     }
 }
 
+// A value that the compiler cannot compute ahead: what the rare branches of a loop need
+// would otherwise sit in registers throughout it.
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// block of a page that slot `slot` lies in: exact for pages below 2^20 keys
+__device__ __forceinline__ uint32_t block_of(const Params& p, int slot) {
+    return p.cs.block == 16 ? slot >> 4 : (uint32_t)(((uint64_t)(uint32_t)(slot >> 4) * p.per_block) >> 32);
+}
+
 __device__ __forceinline__ int clamp_page(const Params& p, int page) { return min(max(page, 0), p.cs.num_pages - 1); }
+
+// Which tiles a wave of a worker takes (those of this place, every W).  The workers of a CU
+// differ, so that few tiles leave no SIMD of it idle.
+template <int W>
+__device__ __forceinline__ int place(int wave) {
+    return W == 1 ? 0 : (wave + 2 * (int)(blockIdx.x / kRangeCUs)) % W;
+}
 
 // The rows of a chunk over the same steps key by key on the vector ALUs, where the
 // products came out non-finite: a product over 16 rows and 32 keys also multiplies the
 // keys that a row does not see, by a probability of 0, and 0 times a non-finite value
 // is NaN.  Every row takes only its own keys here, as the vector-ALU kernels do.
-template <bool F32, int CH, int NT>
+template <bool F32, int CH, int W, int T>
 __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const int g, const int rc, const int q0,
                                             const int ql, const int kv, const int s0, const int s1, const int ns,
                                             const int64_t slot) {
-    typedef Cfg<F32, CH, NT> C;
-    typedef typename std::conditional<F32, float, uint16_t>::type T;
+    typedef Cfg<F32, CH, W, T> C;
+    typedef typename std::conditional<F32, float, uint16_t>::type E;
     constexpr int kPer = (C::Dp + DSPARK_WAVE - 1) / DSPARK_WAVE;  // value dims per lane
     const AttnArgs& a = p.a;
     // (values in vector registers: the scalar ones that this would add to the kernel's
     // are spilled into vector registers that the step loop then lacks)
     int z = 0;
     asm volatile("" : "+v"(z));
-    const int lane = threadIdx.x, page = a.page + z, group = p.group + z, gv = g + z;
-    const int row0 = (rc + z) * (16 * NT), nrows = min(16 * NT, ql * group - row0);
+    const int lane = threadIdx.x & (DSPARK_WAVE - 1), wave = threadIdx.x / DSPARK_WAVE;
+    const int page = a.page + z, group = p.group + z, gv = g + z;
+    const int row0 = (rc + z) * C::Rows, nrows = min(C::Rows, ql * group - row0);
     const int32_t* bt = a.block_table + (int64_t)(r + z) * a.max_pages;
     const uint8_t* kc = (const uint8_t*)a.k + gv * p.ks1;
     const uint8_t* vc = (const uint8_t*)a.v + gv * p.vs1;
     const bool whole = s0 + z == 0 && s1 == ns;
-    float* part = p.part + (slot + z) * ((int64_t)(16 * NT) * (C::Dp + 2));
+    float* part = p.part + (slot + z) * ((int64_t)C::Rows * (C::Dp + 2));
     for (int rr = 0; rr < nrows; ++rr) {
+        if (W > 1 && (rr >> 4) % W != place<W>(wave)) continue;  // the wave's own tiles
         const int row = row0 + rr, t = row / group;
         const int64_t orow = (int64_t)(q0 + t) * a.Hq + gv * group + (row - t * group);
         const int end = min(kv - ql + t + 1, s1 * C::Step);
@@ -181,7 +228,7 @@ __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const 
             const int64_t si = (pg * a.Hkv + gv) * p.nb + at / p.cs.block;
             float sc = 0.0f;
             for (int d = 0; d < a.Dqk + z; ++d)
-                sc += Elem<T>::load((const T*)a.q, orow * a.Dqk + d) * e4m3_to_f32(kr[d]);
+                sc += Elem<E>::load((const E*)a.q, orow * a.Dqk + d) * e4m3_to_f32(kr[d]);
             sc *= p.cs.k[si] * p.scale2;
             if (k0 + lane >= end) sc = -__builtin_huge_valf();
             const float mn = fmaxf(m, wave_max(sc));
@@ -204,7 +251,7 @@ __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const 
             }
         }
         if (lane == 0) {
-            if (!whole) part[rr] = m, part[16 * NT + rr] = l;
+            if (!whole) part[rr] = m, part[C::Rows + rr] = l;
             else if (a.lse) a.lse[orow] = (m + log2f(l)) * kLn2;
         }
         const float inv = 1.0f / l;
@@ -212,78 +259,311 @@ __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const 
         for (int e = 0; e < kPer; ++e) {
             const int d = lane + e * DSPARK_WAVE;
             if (d >= a.Dv) continue;
-            if (whole) Elem<T>::store((T*)a.out, orow * a.Dv + d, o[e] * inv);
-            else part[2 * 16 * NT + rr * C::Dp + d] = o[e];
+            if (whole) Elem<E>::store((E*)a.out, orow * a.Dv + d, o[e] * inv);
+            else part[2 * C::Rows + rr * C::Dp + d] = o[e];
         }
     }
 }
 
-// Steps [s0, s1) of the ns steps of one (request, head, chunk).  `slot`: where
-// the partial goes when they are not all of them.  Returns whether a sum of its rows is
-// not finite (what is written is then not yet the result).
-template <bool F32, int CH, int NT>
-__device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
-                                       const int q0, const int ql, const int kv, const int s0, const int s1,
-                                       const int ns, const int64_t slot) {
-    typedef Cfg<F32, CH, NT> C;
-    constexpr int S = C::S, H = C::H, P = C::P, TQ = C::TQ, TP = C::TP;
-    constexpr uint32_t kScales = 2 * C::TileB;  // LDS offset of the step's scales
-    const AttnArgs& a = p.a;
-    const int lane = threadIdx.x;
-    const int lr = lane & 15, lq = lane >> 4;
-    const int rows = ql * p.group;
-    const int row0 = rc * (16 * NT);
-    const int nt = min(NT, (rows - row0 + 15) >> 4);
+// N of a wave's row tiles: tile j holds rows first + 16 W j ..
+template <bool F32, int CH, int W, int T, int N>
+struct Tiles {
+    typedef Cfg<F32, CH, W, T> C;
+    static constexpr int S = C::S, H = C::H, DB = C::DB, TQ = C::TQ, TP = C::TP;
 
-    // ---- query fragments (B operand of S^T = K Q^T) and causal limits: slice 2 i + h holds
-    // dims 64 i + 16 lq + 8 h ..
-    u32x4 qf[NT][2 * S][TQ];
-    int lim[NT];
-    int lim_min = 0x7fffffff;
+    u32x4 qf[N][2 * S][TQ];  // queries, B operand: slice 2 i + h holds dims 64 i + 16 lq + 8 h ..
+    int lim[N];              // last key that the row sees
+    int lim_min;             // of the wave's rows
+    f32x4 acc[N][DB];        // bf16: of v * s_v / vref
+    float m[N], l[N];        // reference of the scores; sum of the probabilities
+    float vref, vinv;        // bf16: a power of two that the values' scales stay below
+
+    __device__ __forceinline__ void load(const Params& p, int g, int first, int q0, int ql, int kv) {
+        const AttnArgs& a = p.a;
+        const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
+        const int rows = ql * p.group;
+        lim_min = 0x7fffffff;
+        vref = 0.0f;
+        vinv = 1.0f;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int row = row0 + 16 * j + lr;
-        lim[j] = -1;
-#pragma unroll
-        for (int s = 0; s < 2 * S; ++s)
-#pragma unroll
-            for (int t = 0; t < TQ; ++t) qf[j][s][t] = u32x4{0u, 0u, 0u, 0u};
-        if (row < rows) {
+        for (int j = 0; j < N; ++j) {
+            const int row = first + 16 * W * j + lr;
             const int t = row / p.group;
             const int h = g * p.group + (row - t * p.group);
             const int64_t at = ((int64_t)(q0 + t) * a.Hq + h) * a.Dqk;
+            const bool in = row < rows;
+            lim[j] = in ? kv - ql + t : -1;
+            if (in) lim_min = min(lim_min, lim[j]);
+            m[j] = -__builtin_huge_valf();
+            l[j] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[j][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < 2 * S; ++s) {
                 const int d = 64 * (s >> 1) + 16 * lq + 8 * (s & 1);
-                if (d >= a.Dqk) continue;
+                const bool ok = in && d < a.Dqk;
                 if constexpr (F32) {
-                    const f32x4 lo = *(const f32x4*)((const float*)a.q + at + d), hi = *(const f32x4*)((const float*)a.q + at + d + 4);
+                    f32x4 x[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+                    if (ok) {
+                        x[0] = *(const f32x4*)((const float*)a.q + at + d);
+                        x[1] = *(const f32x4*)((const float*)a.q + at + d + 4);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         uint32_t w[TQ];
-                        terms<TQ>(e < 2 ? lo[2 * e] : hi[2 * e - 4], e < 2 ? lo[2 * e + 1] : hi[2 * e - 3], w);
+                        terms<TQ>(x[e >> 1][2 * (e & 1)], x[e >> 1][2 * (e & 1) + 1], w);
 #pragma unroll
-                        for (int x = 0; x < TQ; ++x) qf[j][s][x][e] = w[x];
+                        for (int y = 0; y < TQ; ++y) qf[j][s][y][e] = w[y];
                     }
                 } else {
-                    qf[j][s][0] = *(const u32x4*)((const uint16_t*)a.q + at + d);
+                    qf[j][s][0] = u32x4{0u, 0u, 0u, 0u};
+                    if (ok) qf[j][s][0] = *(const u32x4*)((const uint16_t*)a.q + at + d);
                 }
             }
-            lim[j] = kv - ql + t;
-            lim_min = min(lim_min, lim[j]);
+        }
+        lim_min = __reduce_min_sync(~0ull, lim_min);
+    }
+
+    // Scores of a step's keys (half h: keys key0 + 32 h + 8 lq + 4 mb + e of row lr), and from
+    // them the probabilities times the values' scales.  FULL: every row sees every key.
+    // vscale[h]: of the lane's eight keys of the half, and of the other sixteen's block.
+    template <bool FULL>
+    __device__ __forceinline__ void scores(const Params& p, const u32x4 (&kf)[H][2][S], const float (&kscale)[H],
+                                           const float (&vscale)[H][2], int key0, int kv, u32x4 (&pb)[H][N][TP]) {
+        const int lq = (here(threadIdx.x) & 63) >> 4;
+        f32x4 sc[N][H][2];
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int h = 0; h < H; ++h) sc[j][h][0] = sc[j][h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int h = 0; h < H; ++h)
+#pragma unroll
+                    for (int mb = 0; mb < 2; ++mb) {
+                        const bf16x8 k = widen(kf[h][mb][i][2 * x], kf[h][mb][i][2 * x + 1]);
+#pragma unroll
+                        for (int t = 0; t < TQ; ++t)
+#pragma unroll
+                            for (int j = 0; j < N; ++j)
+                                sc[j][h][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                    k, __builtin_bit_cast(bf16x8, qf[j][2 * i + x][t]), sc[j][h][mb], 0, 0, 0);
+                    }
+        // The eight keys of a lane have one scale, so their maximum is taken before it
+        // (where a scale is negative this is the least of them: a reference too low,
+        // which at worst overflows and is computed again)
+        float bm[N], ks[H], vs[H], most = 0.0f;
+        bool need = false;
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            ks[h] = kscale[h] * p.scale2;
+            vs[h] = vscale[h][0];
+            if constexpr (!F32)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const float y = __builtin_fabsf(vscale[h][x]);
+                    if (y < __builtin_huge_valf()) most = fmaxf(most, y);
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            bm[j] = -__builtin_huge_valf();
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                f32x4 &x = sc[j][h][0], &y = sc[j][h][1];
+                if constexpr (!FULL) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = key0 + 32 * h + 8 * lq + e;
+                        x[e] = key < kv && key <= lim[j] ? x[e] * ks[h] : -__builtin_huge_valf();
+                        y[e] = key + 4 < kv && key + 4 <= lim[j] ? y[e] * ks[h] : -__builtin_huge_valf();
+                    }
+                }
+                float b = vmax(vmax(x[0], x[1]), x[2]);  // (three operands an instruction)
+                b = vmax(vmax(b, x[3]), y[0]);
+                b = vmax(vmax(b, y[1]), y[2]);
+                b = vmax(b, y[3]);
+                if constexpr (FULL) b *= ks[h];
+                bm[j] = h ? vmax(bm[j], b) : b;
+            }
+            bm[j] = row_max4(bm[j]);
+            need = need || bm[j] > m[j] + Ref<F32>::kHead;
+        }
+        // fp16 holds p * s_v only relative to the largest s_v so far
+        const bool vneed = !F32 && most > vref;
+        if (__builtin_amdgcn_ballot_w64(need || vneed)) {
+            float f = 1.0f;
+            if (vneed) {  // (alike in all lanes)
+                const float up = __uint_as_float(min((__float_as_uint(most) + 0x7fffffu) & 0x7f800000u, 0x7e800000u));
+                f = vref / up;
+                vref = up;
+                vinv = 1.0f / up;
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const bool up = bm[j] > m[j] + Ref<F32>::kHead;
+                const float mn = up ? bm[j] - Ref<F32>::kBias : m[j];
+                const float alpha = up ? __builtin_amdgcn_exp2f(m[j] - mn) : 1.0f;
+                l[j] *= alpha;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) acc[j][d] *= alpha * f;
+                m[j] = mn;
+            }
+        }
+        if constexpr (!F32)
+#pragma unroll
+            for (int h = 0; h < H; ++h) vs[h] *= vinv;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float mu = m[j] == -__builtin_huge_valf() ? 0.0f : m[j];
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                float pr[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const float s = sc[j][h][x >> 2][x & 3];
+                    pr[x] = __builtin_amdgcn_exp2f(FULL ? __builtin_fmaf(s, ks[h], -mu) : s - mu);
+                }
+                l[j] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+#pragma unroll
+                for (int x = 0; x < 8; ++x)  // (a masked key's scale may be anything)
+                    pr[x] = FULL || sc[j][h][x >> 2][x & 3] != -__builtin_huge_valf() ? pr[x] * vs[h] : 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (F32) {
+                        uint32_t w[TP];
+                        terms<TP>(pr[2 * e], pr[2 * e + 1], w);
+#pragma unroll
+                        for (int t = 0; t < TP; ++t) pb[h][j][t][e] = w[t];
+                    } else {
+                        pb[h][j][0][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{pr[2 * e], pr[2 * e + 1]}), f16x2));
+                    }
+                }
+            }
         }
     }
-    lim_min = __reduce_min_sync(~0ull, lim_min);
 
-    f32x4 acc[NT][C::DB];
-    float mrow[NT], lsum[NT];
+    // O^T += V^T P^T; vf: dims 16 d + lr, the lane's keys of a half
+    __device__ __forceinline__ void values(const i32x2 (&vf)[DB], const u32x4 (&pb)[N][TP]) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        mrow[j] = -__builtin_huge_valf();
-        lsum[j] = 0.0f;
+        for (int d = 0; d < DB; ++d) {
+            if constexpr (F32) {
+                const bf16x8 v = widen(vf[d][0], vf[d][1]);
 #pragma unroll
-        for (int d = 0; d < C::DB; ++d) acc[j][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int t = 0; t < TP; ++t)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        acc[j][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, pb[j][t]), acc[j][d], 0, 0, 0);
+            } else {
+                const f16x8 v = widen_half(vf[d][0], vf[d][1]);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    acc[j][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, __builtin_bit_cast(f16x8, pb[j][0]), acc[j][d], 0, 0, 0);
+            }
+        }
     }
+
+    // The rows' results, or their partials.  Returns whether a sum of them is not finite
+    // (what is written is then not yet the result).
+    __device__ __forceinline__ bool finish(const Params& p, int g, int row0, int first, int q0, int ql, bool whole,
+                                           float* part) {
+        const AttnArgs& a = p.a;
+        const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
+        float big[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // largest sum by magnitude (NaN if one is), in independent chains
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            // total l over the four lanes of a row
+            l[j] += __shfl_xor(l[j], 16, 64);
+            l[j] += __shfl_xor(l[j], 32, 64);
+            const int row = first + 16 * W * j + lr, rr = row - row0;
+            if (row >= ql * p.group) continue;
+            big[0] = vmax(big[0], l[j]);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                big[d & 3] = vmax(vmax(__builtin_fabsf(acc[j][d][0]), __builtin_fabsf(acc[j][d][1])), big[d & 3]);
+                big[d & 3] = vmax(vmax(__builtin_fabsf(acc[j][d][2]), __builtin_fabsf(acc[j][d][3])), big[d & 3]);
+            }
+            const int t = row / p.group;
+            const int64_t orow = (int64_t)(q0 + t) * a.Hq + g * p.group + (row - t * p.group);
+            if constexpr (!F32) {
+#pragma unroll
+                for (int d = 0; d < DB; ++d) acc[j][d] *= vref;
+            }
+            const float inv = 1.0f / l[j];
+            if (whole) {
+                if (a.lse && lq == 0) a.lse[orow] = (m[j] + log2f(l[j])) * kLn2;
+            } else if (lq == 0) {
+                part[rr] = m[j];
+                part[C::Rows + rr] = l[j];
+            }
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const int dim = 16 * d + 4 * lq;  // four consecutive dims of this lane
+                const f32x4 o = acc[j][d];
+                if (!whole) {
+                    *(f32x4*)(part + 2 * C::Rows + (int64_t)rr * C::Dp + dim) = o;
+                } else if (dim < a.Dv) {
+                    if (F32) *(f32x4*)((float*)a.out + orow * a.Dv + dim) = o * inv;
+                    else
+                        *(uint2*)((uint16_t*)a.out + orow * a.Dv + dim) =
+                            uint2{pack2_bf16(o[0] * inv, o[1] * inv), pack2_bf16(o[2] * inv, o[3] * inv)};
+                }
+            }
+        }
+        return __builtin_amdgcn_ballot_w64(!(vmax(vmax(big[0], big[1]), vmax(big[2], big[3])) < __builtin_huge_valf())) != 0;
+    }
+};
+
+// LDS addresses of the operand reads in the first buffer (the second half of a step and
+// the key block are immediate offsets: the swizzles leave bits 2 and 5 of the key alone)
+template <typename C, int CH>
+struct Reads {
+    uint32_t k[C::S], v, scale;
+    __device__ __forceinline__ void set(uint32_t lds0) {
+        const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < C::S; ++i) {
+            const int t = 8 * (lr >> 2) + (lr & 3);
+            k[i] = lds0 + t * C::RowB + 16 * k_slot<CH>(t, 4 * i + lq);
+        }
+        const int t = 8 * lq + (lr >> 1);
+        v = lds0 + C::TileB + t * C::RowB + 16 * v_slot<CH>(t, 0) + 8 * (lr & 1);
+        scale = lds0 + 2 * C::TileB + (lq >> 1) * C::ScaleStep;
+    }
+    __device__ __forceinline__ void keys(uint32_t buf, int h, u32x4 (&kf)[2][C::S], float& ks, float (&vs)[2]) const {
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+            for (int i = 0; i < C::S; ++i)
+                kf[mb][i] = *lds_ptr<const lds_u32x4>(k[i] + buf + (32 * h + 4 * mb) * C::RowB);
+        ks = *lds_ptr<const lds_f32>(scale + buf + 2 * h * C::ScaleStep);
+        vs[0] = *lds_ptr<const lds_f32>(scale + buf + 2 * h * C::ScaleStep + C::ScaleV);
+        vs[1] = *lds_ptr<const lds_f32>(((scale + buf) ^ C::ScaleStep) + 2 * h * C::ScaleStep + C::ScaleV);
+    }
+    __device__ __forceinline__ void values(uint32_t buf, int h, i32x2 (&vf)[C::DB]) const {
+#pragma unroll
+        for (int d = 0; d < C::DB; ++d)
+            // (buffers lie at multiples of 256 bytes: the swizzle's XOR goes through the address)
+            vf[d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(lds_ptr<lds_i32x2>(((v + buf) ^ (16 * d)) + 32 * h * C::RowB));
+    }
+};
+
+// Steps [s0, s1) of the ns steps of one (request, head, chunk) of N row tiles, by a single
+// wave.  `slot`: where the partial goes when they are not all of them.
+template <bool F32, int CH, int T, int N>
+__device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
+                                       const int q0, const int ql, const int kv, const int s0, const int s1,
+                                       const int ns, const int64_t slot) {
+    typedef Cfg<F32, CH, 1, T> C;
+    constexpr int S = C::S, H = C::H, P = C::P;
+    const AttnArgs& a = p.a;
+    const int lane = threadIdx.x;
+    const int row0 = rc * C::Rows;
+    Tiles<F32, CH, 1, T, N> tiles;
+    tiles.load(p, g, row0, q0, ql, kv);
 
     // ---- copy offsets from a piece's first key: instruction i covers chunks 64 i + lane
     // of its 16 rows (the maps are involutions; K's depends on the piece's parity)
@@ -295,21 +575,8 @@ __device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, con
         for (int h = 0; h < 2; ++h) ko[h][i] = t * p.ks2 + 16 * k_slot<CH>(t + 16 * h, c);
         vo[i] = t * p.vs2 + 16 * v_slot<CH>(t, c);
     }
-    // LDS addresses of the operand reads (the second half of a step and the key block are
-    // immediate offsets: the swizzles leave bits 2 and 5 of the key alone)
-    uint32_t kaddr[S];
-#pragma unroll
-    for (int i = 0; i < S; ++i) {
-        const int t = 8 * (lr >> 2) + (lr & 3);
-        kaddr[i] = lds0 + t * C::RowB + 16 * k_slot<CH>(t, 4 * i + lq);
-    }
-    uint32_t vaddr[C::DB];
-#pragma unroll
-    for (int d = 0; d < C::DB; ++d) {
-        const int t = 8 * lq + (lr >> 1);
-        vaddr[d] = lds0 + C::TileB + t * C::RowB + 16 * v_slot<CH>(t, d) + 8 * (lr & 1);
-    }
-    const uint32_t saddr = lds0 + kScales + 4 * (lq >> 1);
+    Reads<C, CH> reads;
+    reads.set(lds0);
     const uint64_t k_head = (uint64_t)(uintptr_t)a.k + (uint64_t)(g * p.ks1);
     const uint64_t v_head = (uint64_t)(uintptr_t)a.v + (uint64_t)(g * p.vs1);
 
@@ -330,58 +597,67 @@ __device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, con
         int ikey = sb * C::Step;
         int ipg = 0, islot = ikey - pg0 * a.page;
         int iblk = islot / p.cs.block, iin = islot - iblk * p.cs.block;  // block of the page, tokens into it
-        uint64_t kslot = (uint64_t)islot * p.ks2, vslot = (uint64_t)islot * p.vs2;  // bytes
         uint64_t vbase[P];
         int vkey = 0;
-        auto copy = [&](uint64_t base, const uint32_t (&off)[S], int piece, int key0, uint32_t dst, auto slot, int bytes) {
-            if (key0 + 16 <= kv && !p.pad) {
+        // the pieces of a step that ends inside the context, rows as wide as LDS's
+        auto copy = [&](const uint64_t (&base)[P], const uint32_t (&even)[S], const uint32_t (&odd)[S], uint32_t dst) {
 #pragma unroll
-                for (int i = 0; i < S; ++i) lds_copy16_s(base, off[i], dst + (piece * S + i) * 1024);
-            } else {
+            for (int h = 0; h < P; ++h)
+#pragma unroll
+                for (int i = 0; i < S; ++i) lds_copy16_s(base[h], h & 1 ? odd[i] : even[i], dst + (h * S + i) * 1024);
+        };
+        // any others: what is not there comes as zeros
+        auto copy_part = [&](const uint64_t (&base)[P], const uint32_t (&even)[S], const uint32_t (&odd)[S], int key0,
+                             uint32_t dst, auto slot, int bytes) {
+            const int ln = here(lane);
+#pragma unroll
+            for (int h = 0; h < P; ++h)
 #pragma unroll
                 for (int i = 0; i < S; ++i) {
-                    const int t = (64 * i + lane) / CH, c = (64 * i + lane) % CH;
-                    const bool in = key0 + t < kv && 16 * slot(t + 16 * (piece & 1), c) < bytes;
-                    lds_copy16(in ? (const void*)(uintptr_t)(base + off[i]) : (const void*)g_zero,
-                               dst + (piece * S + i) * 1024);
+                    const int t = (64 * i + ln) / CH, c = (64 * i + ln) % CH;
+                    const bool in = key0 + 16 * h + t < kv && 16 * slot(t + 16 * (h & 1), c) < bytes;
+                    lds_copy16(in ? (const void*)(uintptr_t)(base[h] + (h & 1 ? odd[i] : even[i])) : (const void*)g_zero,
+                               dst + (h * S + i) * 1024);
                 }
-            }
         };
         auto issue_k = [&]() {
             vkey = ikey;
+            uint64_t kbase[P];
             uint32_t si[P];  // scales of the pieces
 #pragma unroll
             for (int h = 0; h < P; ++h) {
                 const int lo = __builtin_amdgcn_readlane(pgs[0], ipg & 63);
                 const int hi = __builtin_amdgcn_readlane(pgs[1], ipg & 63);
                 const uint32_t page = ipg < DSPARK_WAVE ? lo : hi;
-                vbase[h] = v_head + (uint64_t)page * p.vs0 + vslot;
-                copy(k_head + (uint64_t)page * p.ks0 + kslot, ko[h & 1], h, ikey, lds0, k_slot<CH>, a.Dqk);
+                // (islot * ks2: below 2^31)
+                kbase[h] = k_head + (uint64_t)page * p.ks0 + (uint64_t)((uint32_t)islot * p.ks2);
+                vbase[h] = v_head + (uint64_t)page * p.vs0 + (uint64_t)((uint32_t)islot * p.vs2);
                 si[h] = (page * (uint32_t)a.Hkv + (uint32_t)g) * (uint32_t)p.nb + (uint32_t)iblk;
-                ikey += 16;
                 islot += 16;
                 iin += 16;
-                kslot += 16 * p.ks2;  // 16 keys: below 2^32 bytes
-                vslot += 16 * p.vs2;
                 if (iin >= p.cs.block) {
                     iin = 0;
                     ++iblk;
                 }
                 if (islot >= a.page) {
                     islot = iblk = 0;
-                    kslot = vslot = 0;
                     ++ipg;
                 }
             }
-            // lanes 0 .. P - 1 the keys' scales, the next P the values' (the others again)
+            if (ikey + C::Step <= kv && !p.pad) copy(kbase, ko[0], ko[1], lds0);
+            else copy_part(kbase, ko[0], ko[1], ikey, lds0, k_slot<CH>, a.Dqk);
+            ikey += C::Step;
+            // lanes 0 .. P - 1 the keys' scales, the next P the values' (the others again);
+            // of pieces past the context 0 (what is there may be anything)
             uint32_t mine = si[0];
 #pragma unroll
             for (int h = 1; h < P; ++h) mine = (lane & (P - 1)) == h ? si[h] : mine;
-            lds_copy4((lane & P ? p.cs.v : p.cs.k) + mine, lds0 + kScales);
+            const float* at = (lane & P ? p.cs.v : p.cs.k) + mine;
+            lds_copy4(vkey + 16 * (lane & (P - 1)) < kv ? (const void*)at : (const void*)g_zero, lds0 + 2 * C::TileB);
         };
         auto issue_v = [&]() {
-#pragma unroll
-            for (int h = 0; h < P; ++h) copy(vbase[h], vo, h, vkey + 16 * h, lds0 + C::TileB, v_slot<CH>, a.Dv);
+            if (vkey + C::Step <= kv && !p.pad) copy(vbase, vo, vo, lds0 + C::TileB);
+            else copy_part(vbase, vo, vo, vkey, lds0 + C::TileB, v_slot<CH>, a.Dv);
         };
 
         // ---- the segment.  One K and one V buffer: a buffer is refilled for the
@@ -389,228 +665,237 @@ __device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, con
         // K lands during the softmax and the value product and the next V during
         // the next scores.  Copies land in order: with V (or the next K) issued
         // after it, K (or V) has landed at vmcnt <= the copies of that.
-        wait_copies<0>();
-        issue_k();
-        issue_v();
-        for (int n = 0; n < nseg; ++n) {
-            const int tok0 = (sb + n) * C::Step;
+        auto step = [&](int n, auto fullc) {
             const bool more = n + 1 < nseg;
-            const bool full = tok0 + C::Step <= kv && tok0 + C::Step - 1 <= lim_min;
             wait_copies<P * S>();  // K and scales of step n
-            u32x4 kf[H][2][S];
-            float ksc[H], vsc[H];  // of the lane's eight keys of a half
+            u32x4 kf[H][2][S], pb[H][N][C::TP];
+            float ks[H], vs[H][2];
+            i32x2 vf[H][C::DB];
 #pragma unroll
-            for (int h = 0; h < H; ++h) {
-#pragma unroll
-                for (int mb = 0; mb < 2; ++mb)
-#pragma unroll
-                    for (int i = 0; i < S; ++i)
-                        kf[h][mb][i] = *lds_ptr<const lds_u32x4>(kaddr[i] + (32 * h + 4 * mb) * C::RowB);
-                ksc[h] = *lds_ptr<const lds_f32>(saddr + 8 * h);
-                vsc[h] = *lds_ptr<const lds_f32>(saddr + 8 * h + 4 * P);
-            }
+            for (int h = 0; h < H; ++h) reads.keys(0, h, kf[h], ks[h], vs[h]);
             wait_lds();
             if (more) issue_k();
-            // scores: half h, keys tok0 + 32 h + 8 lq + 4 mb + e of query row lr
-            f32x4 sc[NT][H][2];
-#pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int mb = 0; mb < 2; ++mb) {
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) sc[j][h][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int i = 0; i < S; ++i)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const bf16x8 k = widen(kf[h][mb][i][2 * x], kf[h][mb][i][2 * x + 1]);
-#pragma unroll
-                            for (int j = 0; j < NT; ++j) {
-                                if (j > 0 && j >= nt) continue;
-#pragma unroll
-                                for (int t = 0; t < TQ; ++t)
-                                    sc[j][h][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                        k, __builtin_bit_cast(bf16x8, qf[j][2 * i + x][t]), sc[j][h][mb], 0, 0, 0);
-                            }
-                        }
-                }
-            u32x4 pb[NT][H][TP];  // probabilities times the values' scales
-#pragma unroll
-            for (int h = 0; h < H; ++h) ksc[h] *= p.scale2;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if (j > 0 && j >= nt) continue;
-                float sv[H][8];
-#pragma unroll
-                for (int h = 0; h < H; ++h)
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) sv[h][x] = sc[j][h][x >> 2][x & 3] * ksc[h];
-                if (!full) {
-#pragma unroll
-                    for (int h = 0; h < H; ++h)
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) {
-                            const int key = tok0 + 32 * h + 8 * lq + x;
-                            if (!(key < kv && key <= lim[j])) sv[h][x] = -__builtin_huge_valf();
-                        }
-                }
-                float bm = -__builtin_huge_valf();
-#pragma unroll
-                for (int h = 0; h < H; ++h)
-                    bm = vmax(bm, vmax(vmax(vmax(sv[h][0], sv[h][1]), vmax(sv[h][2], sv[h][3])),
-                                       vmax(vmax(sv[h][4], sv[h][5]), vmax(sv[h][6], sv[h][7]))));
-                bm = row_max4(bm);
-                const bool need = bm > mrow[j] + kRescale;
-                if (__builtin_amdgcn_ballot_w64(need)) {
-                    const float mn = need ? bm : mrow[j];
-                    const float alpha = need ? __builtin_amdgcn_exp2f(mrow[j] - mn) : 1.0f;
-                    lsum[j] *= alpha;
-#pragma unroll
-                    for (int d = 0; d < C::DB; ++d) acc[j][d] *= alpha;
-                    mrow[j] = mn;
-                }
-                const float mu = mrow[j] == -__builtin_huge_valf() ? 0.0f : mrow[j];
-#pragma unroll
-                for (int h = 0; h < H; ++h) {
-                    float pr[8];
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) pr[x] = __builtin_amdgcn_exp2f(sv[h][x] - mu);
-                    lsum[j] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
-                    if (full) {
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) pr[x] *= vsc[h];
-                    } else {  // (a masked key's scale may be anything)
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) pr[x] = sv[h][x] == -__builtin_huge_valf() ? 0.0f : pr[x] * vsc[h];
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        uint32_t w[TP];
-                        terms<TP>(pr[2 * e], pr[2 * e + 1], w);
-#pragma unroll
-                        for (int t = 0; t < TP; ++t) pb[j][h][t][e] = w[t];
-                    }
-                }
-            }
+            tiles.template scores<decltype(fullc)::value>(p, kf, ks, vs, (sb + n) * C::Step, kv, pb);
             if (more) wait_copies<P * S + 1>();  // V of step n
             else wait_copies<0>();
-            i32x2 vf[H][C::DB];  // dims 16 d + lr, keys 32 h + 8 lq ..
 #pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int d = 0; d < C::DB; ++d)
-                    vf[h][d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(lds_ptr<lds_i32x2>(vaddr[d] + 32 * h * C::RowB));
+            for (int h = 0; h < H; ++h) reads.values(0, h, vf[h]);
             wait_lds();
             if (more) issue_v();
 #pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int d = 0; d < C::DB; ++d) {
-                    const bf16x8 v = widen(vf[h][d][0], vf[h][d][1]);
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) {
-                        if (j > 0 && j >= nt) continue;
-#pragma unroll
-                        for (int t = 0; t < TP; ++t)
-                            acc[j][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                v, __builtin_bit_cast(bf16x8, pb[j][h][t]), acc[j][d], 0, 0, 0);
-                    }
-                }
-        }
+            for (int h = 0; h < H; ++h) tiles.values(vf[h], pb[h]);
+        };
+        wait_copies<0>();
+        issue_k();
+        issue_v();
+        // steps that every row sees whole, then the rest
+        const int full = max(0, min(nseg, min(kv, tiles.lim_min + 1) / C::Step - sb));
+        int n = 0;
+        for (; n < full; ++n) step(n, std::true_type{});
+        for (; n < nseg; ++n) step(n, std::false_type{});
         sb = se;
     }
-
-    // ---- rows: total l over the four lanes of a row
-    const bool whole = s0 == 0 && s1 == ns;
-    float* part = p.part + slot * ((int64_t)(16 * NT) * (C::Dp + 2));
-    float big[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // largest sum by magnitude (NaN if one is), in independent chains
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        lsum[j] += __shfl_xor(lsum[j], 16, 64);
-        lsum[j] += __shfl_xor(lsum[j], 32, 64);
-        const int rr = 16 * j + lr, row = row0 + rr;
-        if (row >= rows) continue;
-        big[0] = vmax(big[0], lsum[j]);
-#pragma unroll
-        for (int d = 0; d < C::DB; ++d) {
-            big[d & 3] = vmax(vmax(__builtin_fabsf(acc[j][d][0]), __builtin_fabsf(acc[j][d][1])), big[d & 3]);
-            big[d & 3] = vmax(vmax(__builtin_fabsf(acc[j][d][2]), __builtin_fabsf(acc[j][d][3])), big[d & 3]);
-        }
-        const int t = row / p.group;
-        const int64_t orow = (int64_t)(q0 + t) * a.Hq + g * p.group + (row - t * p.group);
-        const float inv = 1.0f / lsum[j];
-        if (whole) {
-            if (a.lse && lq == 0) a.lse[orow] = (mrow[j] + log2f(lsum[j])) * kLn2;
-        } else if (lq == 0) {
-            part[rr] = mrow[j];
-            part[16 * NT + rr] = lsum[j];
-        }
-#pragma unroll
-        for (int d = 0; d < C::DB; ++d) {
-            const int dim = 16 * d + 4 * lq;  // four consecutive dims of this lane
-            const f32x4 o = acc[j][d];
-            if (!whole) {
-                *(f32x4*)(part + 2 * 16 * NT + (int64_t)rr * C::Dp + dim) = o;
-            } else if (dim < a.Dv) {
-                if (F32) *(f32x4*)((float*)a.out + orow * a.Dv + dim) = o * inv;
-                else
-                    *(uint2*)((uint16_t*)a.out + orow * a.Dv + dim) =
-                        uint2{pack2_bf16(o[0] * inv, o[1] * inv), pack2_bf16(o[2] * inv, o[3] * inv)};
-            }
-        }
-    }
-    return __builtin_amdgcn_ballot_w64(!(vmax(vmax(big[0], big[1]), vmax(big[2], big[3])) < __builtin_huge_valf())) != 0;
+    return tiles.finish(p, g, row0, row0, q0, ql, s0 == 0 && s1 == ns, p.part + slot * ((int64_t)C::Rows * (C::Dp + 2)));
 }
 
-template <bool F32, int CH, int NT>
-__global__ __launch_bounds__(DSPARK_WAVE) __attribute__((amdgpu_waves_per_eu(Cfg<F32, CH, NT>::Eu)))
+// The same by W waves that share the keys and values, N row tiles in this one (maybe
+// none).  Each wave copies its part of a step, Ring - 1 steps ahead, into a ring of
+// buffers; one barrier a step.
+template <bool F32, int CH, int W, int T, int N>
+__device__ __forceinline__ bool attend_shared(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
+                                              const int q0, const int ql, const int kv, const int s0, const int s1,
+                                              const int ns, const int64_t slot) {
+    typedef Cfg<F32, CH, W, T> C;
+    constexpr int S = C::S, H = C::H, P = C::P, R = C::Ring;
+    constexpr int kOps = P * S / W;  // copies of a wave for a step's keys, and for its values
+    static_assert(P * S % W == 0 && (kOps <= S || kOps % S == 0) && S % (kOps < S ? kOps : S) == 0, "a wave's copies");
+    static_assert(kOps <= S, "a wave's copies lie in one piece");
+    const AttnArgs& a = p.a;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row0 = rc * C::Rows, first = row0 + 16 * place<W>(wave);
+    Tiles<F32, CH, W, T, (N > 0 ? N : 1)> tiles;
+    if constexpr (N > 0) tiles.load(p, g, first, q0, ql, kv);
+
+    // this wave's copies: instructions i0 .. of piece `piece`, and that piece's scales (into
+    // 256 bytes of the wave's own; waves of one piece both copy them)
+    const int piece = kOps * wave / S, i0 = kOps * wave % S;
+    uint32_t ko[kOps], vo[kOps];
+#pragma unroll
+    for (int i = 0; i < kOps; ++i) {
+        const int at = 64 * (i0 + i) + lane, t = at / CH, c = at % CH;
+        ko[i] = t * p.ks2 + 16 * k_slot<CH>(t + 16 * (piece & 1), c);
+        vo[i] = t * p.vs2 + 16 * v_slot<CH>(t, c);
+    }
+    const uint32_t dst0 = lds0 + (piece * S + i0) * 1024, sdst0 = lds0 + 2 * C::TileB + 256 * wave;
+    Reads<C, CH> reads;
+    reads.set(lds0);
+    const uint64_t k_head = (uint64_t)(uintptr_t)a.k + (uint64_t)(g * p.ks1);
+    const uint64_t v_head = (uint64_t)(uintptr_t)a.v + (uint64_t)(g * p.vs1);
+    const uint64_t s_base = (uint64_t)(uintptr_t)(lane & 1 ? p.cs.v : p.cs.k);
+
+    for (int sb = s0; sb < s1;) {
+        const int pg0 = sb * C::Step / a.page;
+        const int pg_last = (kv - 1) / a.page;
+        const int64_t seg_end = (int64_t)(pg0 + kPageRegs * DSPARK_WAVE) * a.page / C::Step;
+        const int se = (int)min((int64_t)s1, seg_end);
+        int pgs[kPageRegs];
+#pragma unroll
+        for (int k = 0; k < kPageRegs; ++k) {
+            const int pg = pg0 + k * DSPARK_WAVE + lane;
+            pgs[k] = pg <= pg_last ? clamp_page(p, a.block_table[(int64_t)r * a.max_pages + pg]) : 0;
+        }
+        const int nseg = se - sb;
+        // the piece to issue next: its key, page (relative) and slot
+        int ikey = sb * C::Step + 16 * piece;
+        int ipg = 0, islot = ikey - pg0 * a.page;
+        uint32_t ibuf = 0;
+        // Every wave issues the same number of copies for every step, in order, also past the
+        // last one (into buffers that are not read again), so a step has landed at a fixed
+        // count.
+        auto issue = [&]() {
+            while (islot >= a.page) {  // (pages are multiples of 16 keys, as pieces are)
+                islot -= a.page;
+                ++ipg;
+            }
+            const int lo = __builtin_amdgcn_readlane(pgs[0], ipg & 63);
+            const int hi = __builtin_amdgcn_readlane(pgs[1], ipg & 63);
+            const uint32_t page = ipg < DSPARK_WAVE ? lo : hi;  // (past the segment: one that is not used)
+            const uint64_t kb = k_head + (uint64_t)page * p.ks0 + (uint64_t)((uint32_t)islot * p.ks2);
+            const uint64_t vb = v_head + (uint64_t)page * p.vs0 + (uint64_t)((uint32_t)islot * p.vs2);
+            const uint32_t si = (page * (uint32_t)a.Hkv + (uint32_t)g) * (uint32_t)p.nb + block_of(p, islot);
+            const uint32_t kd = dst0 + ibuf, vd = kd + C::TileB;
+            if (ikey + 16 <= kv && !p.pad) {
+#pragma unroll
+                for (int i = 0; i < kOps; ++i) {
+                    lds_copy16_s(kb, ko[i], kd + i * 1024);
+                    lds_copy16_s(vb, vo[i], vd + i * 1024);
+                }
+            } else {
+                const int ln = here(lane);
+#pragma unroll
+                for (int i = 0; i < kOps; ++i) {
+                    const int at = 64 * (i0 + i) + ln, t = at / CH, c = at % CH;
+                    const bool in = ikey + t < kv;
+                    const bool ik = in && 16 * k_slot<CH>(t + 16 * (piece & 1), c) < a.Dqk;
+                    const bool iv = in && 16 * v_slot<CH>(t, c) < a.Dv;
+                    lds_copy16(ik ? (const void*)(uintptr_t)(kb + ko[i]) : (const void*)g_zero, kd + i * 1024);
+                    lds_copy16(iv ? (const void*)(uintptr_t)(vb + vo[i]) : (const void*)g_zero, vd + i * 1024);
+                }
+            }
+            // (of a piece past the context 0: what is there may be anything)
+            lds_copy4(ikey < kv ? (const void*)(uintptr_t)(s_base + 4ull * si) : (const void*)g_zero, sdst0 + ibuf);
+            ikey += C::Step;
+            islot += C::Step;
+            ibuf = ibuf == (R - 1) * C::BufB ? 0 : ibuf + C::BufB;
+        };
+        uint32_t buf = 0;
+        auto step = [&](int n, auto fullc) {
+            wait_copies<(R - 2) * (2 * kOps + 1)>();
+            lds_barrier();  // step n is there for all, and everyone is done with step n - 1
+            issue();
+            if constexpr (N > 0) {
+                u32x4 kf[H][2][S], pb[H][N][C::TP];
+                float ks[H], vs[H][2];
+                i32x2 vf[H][C::DB];
+#pragma unroll
+                for (int h = 0; h < H; ++h) reads.keys(buf, h, kf[h], ks[h], vs[h]);
+                tiles.template scores<decltype(fullc)::value>(p, kf, ks, vs, (sb + n) * C::Step, kv, pb);
+#pragma unroll
+                for (int h = 0; h < H; ++h) reads.values(buf, h, vf[h]);
+#pragma unroll
+                for (int h = 0; h < H; ++h) tiles.values(vf[h], pb[h]);
+            }
+            buf = buf == (R - 1) * C::BufB ? 0 : buf + C::BufB;
+        };
+        wait_copies<0>();
+        lds_barrier();  // everyone is done with the buffers
+#pragma unroll
+        for (int n = 0; n < R - 1; ++n) issue();
+        int full = 0;
+        if constexpr (N > 0) full = max(0, min(nseg, min(kv, tiles.lim_min + 1) / C::Step - sb));
+        int n = 0;
+        for (; n < full; ++n) step(n, std::true_type{});
+        for (; n < nseg; ++n) step(n, std::false_type{});
+        wait_copies<0>();
+        sb = se;
+    }
+    if constexpr (N > 0)
+        return tiles.finish(p, g, row0, first, q0, ql, s0 == 0 && s1 == ns,
+                            p.part + slot * ((int64_t)C::Rows * (C::Dp + 2)));
+    return false;
+}
+
+template <bool F32, int CH, int W, int T>
+__global__ __launch_bounds__(DSPARK_WAVE * W) __attribute__((amdgpu_waves_per_eu(Cfg<F32, CH, W, T>::Eu)))
 void attn_scaled_kernel(Params p) {
-    typedef Cfg<F32, CH, NT> C;
-    __shared__ __align__(16) unsigned char lds[C::LdsB];
+    typedef Cfg<F32, CH, W, T> C;
+    __shared__ __align__(256) unsigned char lds[C::LdsB];
     uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0];
     asm volatile("" : "+s"(lds0));
+    const int wave = place<W>(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
     bool again = false;
-    range_walk<C::Step>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
-        again |= attend<F32, CH, NT>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
+    range_walk<C::Step, true>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
+        // (a body for each number of tiles: tests of it would cut the step into pieces that
+        // the compiler cannot interleave)
+        const int n = (ql * p.group - rc * C::Rows + 15) / 16;  // tiles, of all waves
+        const int mine = (n - wave + W - 1) / W;                // dealt round-robin
+        if constexpr (W == 1) {
+            if constexpr (T > 1)
+                if (mine > 1) return (void)(again |= attend<F32, CH, T, 2>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot));
+            again |= attend<F32, CH, T, 1>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
+        } else {
+            if (mine > 0) again |= attend_shared<F32, CH, W, T, 1>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
+            else attend_shared<F32, CH, W, T, 0>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
+        }
     });
     if (!again) return;
-    // (a walk of its own, so that the step loop above holds none of its registers)
-    __syncthreads();  // what the lanes of the wave wrote above comes before what others write below
-    range_walk<C::Step>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
-        scaled_rows<F32, CH, NT>(p, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
+    // (a walk of its own, so that the step loop above holds none of its registers; a wave
+    // goes over its own rows only)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what the lanes wrote above comes before what others write below
+    range_walk<C::Step, true>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
+        scaled_rows<F32, CH, W, T>(p, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
     });
 }
 
 // ------------------------------------------------------------------ host
 
 struct Geom {
-    int ch, nt, rc_max, direct;
-    int64_t resident, waves;  // ranges; grid of the attention kernel
+    int ch, w, t, rc_max, direct, by_head;
+    int64_t resident, workers;  // ranges; grid of the attention kernel
     size_t part_bytes;
 };
 
 template <typename F>
-static auto with_cfg(bool bf16, int ch, int nt, F f) {
-#define DS_CFG(F32, CH, NT) \
-    return f(std::integral_constant<bool, F32>{}, std::integral_constant<int, CH>{}, std::integral_constant<int, NT>{})
+static auto with_cfg(bool bf16, int ch, int w, int t, F f) {
+#define DS_CFG(F32, CH, W, T)                                                                                    \
+    return f(std::integral_constant<bool, F32>{}, std::integral_constant<int, CH>{}, std::integral_constant<int, W>{}, \
+             std::integral_constant<int, T>{})
     if (bf16) {
         if (ch == 4) {
-            if (nt == 1) DS_CFG(false, 4, 1);
-            if (nt == 2) DS_CFG(false, 4, 2);
-            DS_CFG(false, 4, 4);
+            if (w == 4) DS_CFG(false, 4, 4, 1);
+            if (t == 1) DS_CFG(false, 4, 1, 1);
+            DS_CFG(false, 4, 1, 2);
         }
         if (ch == 8) {
-            if (nt == 1) DS_CFG(false, 8, 1);
-            DS_CFG(false, 8, 2);
+            if (w == 4) DS_CFG(false, 8, 4, 1);
+            if (t == 1) DS_CFG(false, 8, 1, 1);
+            DS_CFG(false, 8, 1, 2);
         }
-        DS_CFG(false, 16, 1);
+        if (w == 4) DS_CFG(false, 16, 4, 1);
+        DS_CFG(false, 16, 1, 1);
     }
     if (ch == 4) {
-        if (nt == 1) DS_CFG(true, 4, 1);
-        DS_CFG(true, 4, 2);
+        if (w == 4) DS_CFG(true, 4, 4, 1);
+        if (t == 1) DS_CFG(true, 4, 1, 1);
+        DS_CFG(true, 4, 1, 2);
     }
-    if (ch == 8) DS_CFG(true, 8, 1);
-    DS_CFG(true, 16, 1);
+    if (ch == 8) {
+        if (w == 4) DS_CFG(true, 8, 4, 1);
+        DS_CFG(true, 8, 1, 1);
+    }
+    if (w == 4) DS_CFG(true, 16, 4, 1);
+    DS_CFG(true, 16, 1, 1);
 #undef DS_CFG
 }
 
@@ -621,20 +906,31 @@ static Geom geom(const AttnArgs& a) {
     const int64_t rows = (int64_t)a.max_q * (a.Hq / a.Hkv);
     const int64_t max_kv = (int64_t)a.max_pages * a.page;
     g.direct = max_kv <= kDirectKeys && (rows + 15) / 16 <= kDirectChunks;
-    // row tiles per wave: as many as a request can fill, up to what the registers hold
-    // (more tiles than these read the keys again, from the last-level cache).  Short
-    // contexts have few waves and are bound by a wave's own chain of steps: one tile.
-    const int most = a.bf16 ? (g.ch == 4 ? 4 : g.ch == 8 ? 2 : 1) : (g.ch == 4 ? 2 : 1);
-    g.nt = g.direct ? 1 : (int)std::min<int64_t>(rows <= 16 ? 1 : rows <= 32 ? 2 : 4, most);
-    g.rc_max = (int)((rows + 16 * g.nt - 1) / (16 * g.nt));
+    // One wave takes up to 16 rows, or 32 in two tiles; above, four waves share the keys and
+    // values.  (us, 8 KV heads, contexts of 1000-3000 keys, one wave / four: 32 rows of
+    // heads of 64 145 / 168, of 128 142 / 147, of 256 188 / 141, fp32 112 / 116, 107 / 110 and
+    // 109 / 149; 48 rows 315 / 183, 205 / 157, 259 / 154, fp32 164 / 143, 147 / 131 and
+    // 150 / 157.  Two tiles a wave of four, 128 requests of 64/8 heads: 136 rows each 650
+    // against 780, but 324 against 283 where a request has 35 on average.)  Short
+    // contexts are bound by a wave's own chain of steps: one wave, one tile.
+    const int alone = g.ch == 16 ? (a.bf16 ? 16 : 48) : 32;
+    g.w = g.direct || rows <= alone ? 1 : 4;
+    g.t = g.w == 1 && !g.direct && rows > 16 && (a.bf16 ? g.ch <= 8 : g.ch == 4) ? 2 : 1;
+    g.rc_max = (int)((rows + 16 * g.w * g.t - 1) / (16 * g.w * g.t));
     const int64_t items = (int64_t)a.R * a.Hkv * g.rc_max;
     g.part_bytes = 0;
-    with_cfg(a.bf16, g.ch, g.nt, [&](auto f32, auto ch, auto nt) {
-        typedef Cfg<decltype(f32)::value, decltype(ch)::value, decltype(nt)::value> C;
+    with_cfg(a.bf16, g.ch, g.w, g.t, [&](auto f32, auto ch, auto w, auto t) {
+        typedef Cfg<decltype(f32)::value, decltype(ch)::value, decltype(w)::value, decltype(t)::value> C;
         const int64_t units = items * ((max_kv + C::Step - 1) / C::Step);
         g.resident = kRangeCUs * C::Cu;
-        g.waves = g.direct ? items : std::min<int64_t>(g.resident, (units + kMinUnits - 1) / kMinUnits);
-        if (!g.direct) g.part_bytes = (size_t)g.waves * 2 * (16 * decltype(nt)::value) * (C::Dp + 2) * sizeof(float);
+        g.workers = g.direct ? items : std::min<int64_t>(g.resident, (units + kMinUnits - 1) / kMinUnits);
+        const int64_t ranges = std::min<int64_t>(g.resident / a.Hkv, units / a.Hkv / kMinUnits) / kXcds * kXcds;
+        g.by_head = !g.direct && a.Hkv > 1 && ranges > 0;
+        if (g.by_head) {
+            g.resident = ranges;
+            g.workers = ranges * a.Hkv;
+        }
+        if (!g.direct) g.part_bytes = (size_t)g.workers * 2 * C::Rows * (C::Dp + 2) * sizeof(float);
         return 0;
     });
     return g;
@@ -647,7 +943,7 @@ bool attn_scaled_shape_ok(const AttnArgs& a) {
     const scaled::Geom g = scaled::geom(a);
     // a request's units and the grid fit 32 bits
     return (int64_t)a.Hkv * g.rc_max * (((int64_t)a.max_pages * a.page + 31) / 32) < (int64_t)1 << 31 &&
-           g.waves < (int64_t)1 << 31 && (int64_t)a.R * a.Hkv < kRangePairs;
+           g.workers < (int64_t)1 << 31 && (int64_t)a.R * a.Hkv < kRangePairs;
 }
 
 bool attn_scaled_supported(const AttnArgs& a, const CacheScales& c) {
@@ -657,6 +953,7 @@ bool attn_scaled_supported(const AttnArgs& a, const CacheScales& c) {
     // 32-bit page strides, offsets inside a 16-key piece and indexes of scales
     const int64_t lim0 = (int64_t)1 << 31, lim2 = (int64_t)1 << 24;
     if (a.ks[0] >= lim0 || a.vs[0] >= lim0 || a.ks[2] >= lim2 || a.vs[2] >= lim2) return false;
+    if (a.page >= 1 << 20 || (int64_t)a.page * std::max(a.ks[2], a.vs[2]) >= lim0) return false;
     if ((int64_t)c.num_pages * a.Hkv >= ((int64_t)1 << 32) / (a.page / c.block)) return false;
     return (uintptr_t)a.q % 16 == 0 && (uintptr_t)a.k % 16 == 0 && (uintptr_t)a.v % 16 == 0 &&
            (uintptr_t)a.out % (a.bf16 ? 8 : 16) == 0;
@@ -673,8 +970,8 @@ hipError_t launch_attn_scaled(const AttnArgs& a, const CacheScales& c, void* ws,
     p.a = a;
     p.cs = c;
     p.group = a.Hq / a.Hkv;
-    p.chunk_rows = 16 * g.nt;
-    p.by_head = 0;
+    p.chunk_rows = 16 * g.w * g.t;
+    p.by_head = g.by_head;
     p.resident = (int)g.resident;
     p.min_units = scaled::kMinUnits;
     p.direct = g.direct;
@@ -686,18 +983,19 @@ hipError_t launch_attn_scaled(const AttnArgs& a, const CacheScales& c, void* ws,
     p.vs2 = (uint32_t)a.vs[2];
     p.pad = a.Dqk != 16 * g.ch || a.Dv != 16 * g.ch;
     p.nb = a.page / c.block;
+    p.per_block = (uint32_t)((((uint64_t)1 << 32) + c.block / 16 - 1) / (c.block / 16));
     p.scale2 = a.scale * scaled::kLog2e;
     p.head = (int64_t*)ws;
     p.part = (float*)((char*)ws + range_head_bytes(a.R));
-    return scaled::with_cfg(a.bf16, g.ch, g.nt, [&](auto f32, auto ch, auto nt) {
+    return scaled::with_cfg(a.bf16, g.ch, g.w, g.t, [&](auto f32, auto ch, auto w, auto t) {
         constexpr bool F = decltype(f32)::value;
-        constexpr int CH = decltype(ch)::value, NT = decltype(nt)::value;
-        typedef scaled::Cfg<F, CH, NT> C;
-        const dim3 grid = g.direct ? dim3((unsigned)(a.R * a.Hkv), (unsigned)g.rc_max) : dim3((unsigned)g.waves);
-        hipLaunchKernelGGL((scaled::attn_scaled_kernel<F, CH, NT>), grid, dim3(DSPARK_WAVE), 0, s, p);
+        constexpr int CH = decltype(ch)::value, W = decltype(w)::value, T = decltype(t)::value;
+        typedef scaled::Cfg<F, CH, W, T> C;
+        const dim3 grid = g.direct ? dim3((unsigned)(a.R * a.Hkv), (unsigned)g.rc_max) : dim3((unsigned)g.workers);
+        hipLaunchKernelGGL((scaled::attn_scaled_kernel<F, CH, W, T>), grid, dim3(DSPARK_WAVE * W), 0, s, p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || g.direct) return e;
-        return launch_merge<F, 16 * NT, C::Dp, C::Step>(p, s);
+        return launch_merge<F, C::Rows, C::Dp, C::Step>(p, s);
     });
 }
 

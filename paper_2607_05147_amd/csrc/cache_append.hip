@@ -29,7 +29,6 @@ constexpr int kApThreads = 256;
 constexpr int kApWaves = kApThreads / DSPARK_WAVE;
 constexpr int kApKeep = 8;                // groups of values a lane keeps
 constexpr int64_t kApGrid = 1 << 20;      // workgroups, at most (they stride over the items)
-constexpr int kMinExp = -100, kMaxExp = 120;  // of a scale: 2^-k and x * 2^-k stay normal
 
 struct ApParams {
     AppendArgs a;
@@ -58,40 +57,23 @@ __device__ __forceinline__ void load_values(const T* p, float (&x)[N]) {
     }
 }
 
-// x * inv as e4m3 codes: saturated at 448, what is not finite becomes NaN
-__device__ __forceinline__ uint32_t to_code2(float a, float b, float inv, uint32_t old, bool high) {
-    auto fit = [&](float x) {
-        const float y = x * inv;
-        return __builtin_fabsf(y) < __builtin_huge_valf() ? __builtin_amdgcn_fmed3f(y, -448.0f, 448.0f) : __builtin_nanf("");
-    };
-    return high ? __builtin_amdgcn_cvt_pk_fp8_f32(fit(a), fit(b), old, true)
-                : __builtin_amdgcn_cvt_pk_fp8_f32(fit(a), fit(b), old, false);
-}
-
 template <int N>
 __device__ __forceinline__ void store_codes(uint8_t* p, const float (&x)[N], float inv) {
     if constexpr (N == 1) {
-        *p = (uint8_t)to_code2(x[0], 0.0f, inv, 0, false);
+        *p = (uint8_t)to_e4m3(x[0], 0.0f, inv, 0, false);
     } else {
         uint2 w;
-        w.x = to_code2(x[2], x[3], inv, to_code2(x[0], x[1], inv, 0, false), true);
-        w.y = to_code2(x[6], x[7], inv, to_code2(x[4], x[5], inv, 0, false), true);
+        w.x = to_e4m3(x[2], x[3], inv, to_e4m3(x[0], x[1], inv, 0, false), true);
+        w.y = to_e4m3(x[6], x[7], inv, to_e4m3(x[4], x[5], inv, 0, false), true);
         *(uint2*)p = w;
     }
 }
 
-// exponent of the smallest power of two with a <= 448 * 2^k (448 = 0.875 * 2^9)
-__device__ __forceinline__ int scale_exp(float a) {
-    const uint32_t u = __float_as_uint(a);
-    const int k = (int)(u >> 23) - 126 - 9 + ((u & 0x7fffffu) > 0x600000u);
-    return min(max(k, kMinExp), kMaxExp);
-}
-
-// ... with s <= 2^k
+// exponent of the smallest power of two that is not below s
 __device__ __forceinline__ int ceil_exp(float s) {
     const uint32_t u = __float_as_uint(s);
     const int k = (int)(u >> 23) - 127 + ((u & 0x7fffffu) != 0);
-    return min(max(k, kMinExp), kMaxExp);
+    return min(max(k, kMinScaleExp), kMaxScaleExp);
 }
 
 template <typename T, int N>
@@ -150,7 +132,7 @@ __global__ __launch_bounds__(kApThreads) void cache_append(ApParams p) {
 
         int e = 0x7fffffff;  // of the scale
         const float so = __builtin_fabsf(s_old);
-        if (most > 0.0f) e = scale_exp(most);
+        if (most > 0.0f) e = e4m3_scale_exp(most);
         if (so > 0.0f && so < __builtin_huge_valf()) e = e == 0x7fffffff ? ceil_exp(so) : max(e, ceil_exp(so));
         if (e == 0x7fffffff) e = 0;  // nothing but zeros (or nothing finite)
         const float s = __uint_as_float((uint32_t)(e + 127) << 23), inv = __uint_as_float((uint32_t)(127 - e) << 23);

@@ -38,6 +38,26 @@ template <> struct Elem<uint16_t> {
 // 448; 0x7f is NaN), the low byte of `b`.
 __device__ __forceinline__ float e4m3_to_f32(uint32_t b) { return __builtin_amdgcn_cvt_f32_fp8(b, 0); }
 
+// x * f as e4m3 codes, to nearest even, in the low or the high half of `old`: saturated at
+// 448, what is not finite becomes NaN.
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float f, uint32_t old, bool high) {
+    auto fit = [&](float x) {
+        const float y = x * f;
+        return __builtin_fabsf(y) < __builtin_huge_valf() ? __builtin_amdgcn_fmed3f(y, -448.0f, 448.0f) : __builtin_nanf("");
+    };
+    return high ? __builtin_amdgcn_cvt_pk_fp8_f32(fit(a), fit(b), old, true)
+                : __builtin_amdgcn_cvt_pk_fp8_f32(fit(a), fit(b), old, false);
+}
+
+// Exponent k of the smallest power of two with a <= 448 * 2^k (448 = 0.875 * 2^9), within
+// [-100, 120]: 2^-k and x * 2^-k stay normal.
+constexpr int kMinScaleExp = -100, kMaxScaleExp = 120;
+__device__ __forceinline__ int e4m3_scale_exp(float a) {
+    const uint32_t u = __float_as_uint(a);
+    const int k = (int)(u >> 23) - 126 - 9 + ((u & 0x7fffffu) > 0x600000u);
+    return min(max(k, kMinScaleExp), kMaxScaleExp);
+}
+
 // Wave-wide reductions over 64 lanes (every lane gets the result).
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
