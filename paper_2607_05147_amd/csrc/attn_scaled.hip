@@ -604,7 +604,11 @@ __device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, con
 #pragma unroll
             for (int h = 0; h < P; ++h)
 #pragma unroll
-                for (int i = 0; i < S; ++i) lds_copy16_s(base[h], h & 1 ? odd[i] : even[i], dst + (h * S + i) * 1024);
+                for (int i = 0; i < S; ++i) {
+                    // (a base that the compiler kept in vector registers comes back right before the first copy)
+                    if (i == 0) lds_copy16_s<true>(base[h], h & 1 ? odd[i] : even[i], dst + (h * S + i) * 1024);
+                    else lds_copy16_s(base[h], h & 1 ? odd[i] : even[i], dst + (h * S + i) * 1024);
+                }
         };
         // any others: what is not there comes as zeros
         auto copy_part = [&](const uint64_t (&base)[P], const uint32_t (&even)[S], const uint32_t (&odd)[S], int key0,

@@ -139,16 +139,18 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
 
 // the same with a wave-uniform 64-bit base (SGPRs) and a per-lane 32-bit offset.  The
 // base has to come from scalar arithmetic: a vector instruction's write of it would need
-// five wait states before the copy, which the compiler does not add inside the block.
+// five wait states before the copy, which the compiler does not add inside the block; they
+// are there if Settle.
+template <bool Settle = false>
 __device__ __forceinline__ void lds_copy16_s(uint64_t sbase, uint32_t voff, uint32_t lds_addr) {
     const uint32_t m0 = __builtin_amdgcn_readfirstlane(lds_addr);
     const uint64_t sb = uniform64(sbase);
     asm volatile(
         "s_mov_b32 m0, %0\n\t"
-        "s_nop 0\n\t"
+        "s_nop %3\n\t"
         "global_load_lds_dwordx4 %1, %2"
         :
-        : "s"(m0), "v"(voff), "s"(sb)
+        : "s"(m0), "v"(voff), "s"(sb), "n"(Settle ? 4 : 0)
         : "memory", "m0");
 }
 
