@@ -11,10 +11,16 @@
 // a few tokens at a time, and rolled back, without its values drifting (with
 // s = max / 448 every growth would round the whole block again).
 //
-// An item is one wave: a step brings a request a few rows, 64 lanes x 8 values
-// hold a row of four heads of 128, and nothing waits for another wave.  The new
-// values stay in registers between the maximum and the rounding.  Bound by launch
-// and three dependent loads at a step's sizes, by HBM for prompts.
+// A wave takes a block of one head: a step brings a request a few rows, 64 lanes x 8
+// values hold four rows of 128, and nothing waits for another wave.  The new values
+// stay in registers between the maximum and the rounding (eight passes of 64 x 16
+// bytes, 32 rows of 128 in bf16; more than that is read twice, from L2).  Heads
+// are the fastest index of the grid, so neighbours read one row of the step.  Passes
+// are uniform: with lanes that walked rows and columns on their own the compiler kept
+// an address and a mask a pass (151 registers, three waves a SIMD instead of five).
+//
+// Bound by launch and three dependent loads at a step's sizes (565 rows of 8 heads:
+// 7.0 us), by HBM for prompts: 40000 rows of 8 heads of 128, 246 MB, 76 us, 3.2 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -27,27 +33,30 @@ namespace {
 
 constexpr int kApThreads = 256;
 constexpr int kApWaves = kApThreads / DSPARK_WAVE;
-constexpr int kApKeep = 8;                // groups of values a lane keeps
-constexpr int64_t kApGrid = 1 << 20;      // workgroups, at most (they stride over the items)
+constexpr int kApBlocks = 65535;          // of a grid's third dimension, at most (workgroups stride over the rest)
 
 struct ApParams {
     AppendArgs a;
-    int nblk;       // blocks that a request's rows can reach
-    int sides;      // 2: keys and values, 1: keys alone
-    int64_t items;
+    int nblk;         // blocks that a request's rows can reach
+    int head_groups;  // of kApWaves heads
 };
 
-// N consecutive values of a row, as fp32
+// N consecutive values of a row, as they are there (keep: the compiler does not hold
+// their fp32 forms instead, which are twice as wide)
 template <typename T, int N>
-__device__ __forceinline__ void load_values(const T* p, float (&x)[N]) {
-    if constexpr (N == 1) {
-        x[0] = Elem<T>::load(p, 0);
-    } else if constexpr (std::is_same<T, float>::value) {
-        const float4 lo = *(const float4*)p, hi = *(const float4*)(p + 4);
-        x[0] = lo.x, x[1] = lo.y, x[2] = lo.z, x[3] = lo.w;
-        x[4] = hi.x, x[5] = hi.y, x[6] = hi.z, x[7] = hi.w;
-    } else {
-        const uint4 v = *(const uint4*)p;
+struct Group;
+template <typename T>
+struct Group<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const T* p) { v = *p; }
+    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = Elem<T>::load(&v, 0); }
+    __device__ __forceinline__ void keep() { asm("" : "+v"(v)); }
+};
+template <>
+struct Group<uint16_t, 8> {
+    uint4 v;
+    __device__ __forceinline__ void load(const uint16_t* p) { v = *(const uint4*)p; }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -55,7 +64,18 @@ __device__ __forceinline__ void load_values(const T* p, float (&x)[N]) {
             x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     }
-}
+    __device__ __forceinline__ void keep() { asm("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
+};
+template <>
+struct Group<float, 8> {
+    float4 lo, hi;
+    __device__ __forceinline__ void load(const float* p) { lo = *(const float4*)p, hi = *(const float4*)(p + 4); }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        x[0] = lo.x, x[1] = lo.y, x[2] = lo.z, x[3] = lo.w;
+        x[4] = hi.x, x[5] = hi.y, x[6] = hi.z, x[7] = hi.w;
+    }
+    __device__ __forceinline__ void keep() {}
+};
 
 template <int N>
 __device__ __forceinline__ void store_codes(uint8_t* p, const float (&x)[N], float inv) {
@@ -76,58 +96,77 @@ __device__ __forceinline__ int ceil_exp(float s) {
     return min(max(k, kMinScaleExp), kMaxScaleExp);
 }
 
+// Workgroups: side and four heads, request, block of its new rows.
 template <typename T, int N>
 __global__ __launch_bounds__(kApThreads) void cache_append(ApParams p) {
     const AppendArgs& a = p.a;
     const int lane = threadIdx.x & (DSPARK_WAVE - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / DSPARK_WAVE);
+    const int r = blockIdx.y, side = blockIdx.x / p.head_groups;
+    const int h = (blockIdx.x - side * p.head_groups) * kApWaves + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / DSPARK_WAVE);
+    const int q0 = a.cu_q[r], ql = a.cu_q[r + 1] - q0, kv = a.kv_len[r];
     const int64_t total_rows = min((int64_t)max(a.cu_q[a.R], 0), (int64_t)a.R * a.max_q);
-    for (int64_t it = (int64_t)blockIdx.x * kApWaves + wave; it < p.items; it += (int64_t)gridDim.x * kApWaves) {
-        int64_t id = it;
-        const int h = (int)(id % a.Hkv);
-        id /= a.Hkv;
-        const int side = (int)(id % p.sides);
-        id /= p.sides;
-        const int i = (int)(id % p.nblk), r = (int)(id / p.nblk);
-        const int q0 = a.cu_q[r], ql = a.cu_q[r + 1] - q0, kv = a.kv_len[r];
-        if (ql < 1 || ql > a.max_q || kv < ql || kv > a.max_pages * a.page || q0 < 0 || (int64_t)q0 + ql > total_rows) continue;
-        const int kv0 = kv - ql;
+    if (h >= a.Hkv || ql < 1 || ql > a.max_q || kv < ql || kv > a.max_pages * a.page || q0 < 0 || (int64_t)q0 + ql > total_rows) return;
+    const int kv0 = kv - ql;
+    const int D = side ? a.Dv : a.Dqk;
+    const int64_t ld = side ? a.v_ld : a.k_ld, s0 = side ? a.vs[0] : a.ks[0], s1 = side ? a.vs[1] : a.ks[1], s2 = side ? a.vs[2] : a.ks[2];
+    const T* rows = (const T*)(side ? a.v : a.k) + (int64_t)h * D;
+    uint8_t* cache = (uint8_t*)(side ? a.v_cache : a.k_cache) + h * s1;
+    float* scales = side ? a.v_scale : a.k_scale;
+    // a pass: 64 / width rows of `width` groups of N values (a power of two; of wider rows
+    // 64 groups at a time), so that what changes from pass to pass is the same in every lane
+    const int per = D / N;
+    int width = 64;
+    while (width / 2 >= per) width /= 2;
+    const int lrow = lane / width, lcol = lane % width, rows_of = DSPARK_WAVE / width;
+    const int64_t from0 = lrow * ld + lcol * N, to0 = lrow * s2 + lcol * N;  // this lane's group of the first pass
+    for (int i = blockIdx.z; i < p.nblk; i += gridDim.z) {
         const int lo = (kv0 / a.block + i) * a.block;  // first token of the block
-        if (lo >= kv) continue;
+        if (lo >= kv) return;
         const int pid = a.block_table[(int64_t)r * a.max_pages + lo / a.page];
-        if ((unsigned)pid >= (unsigned)a.num_pages) continue;
-        const int slot = lo % a.page;
         const int first = max(lo, kv0), n = min(kv, lo + a.block) - first;  // new tokens of the block
-        const int D = side ? a.Dv : a.Dqk;
-        const int64_t* st = side ? a.vs : a.ks;
-        const T* src = (const T*)(side ? a.v : a.k) + (int64_t)(q0 + first - kv0) * (side ? a.v_ld : a.k_ld) + (int64_t)h * D;
-        const int64_t ld = side ? a.v_ld : a.k_ld;
-        uint8_t* dst = (uint8_t*)(side ? a.v_cache : a.k_cache) + pid * st[0] + h * st[1] + (int64_t)slot * st[2];
-        float* scale = (side ? a.v_scale : a.k_scale) + ((int64_t)pid * a.Hkv + h) * (a.page / a.block) + slot / a.block;
-        const float s_old = first > lo ? *scale : 0.0f;
-
-        const int per = D / N, groups = n * per;  // groups of N values
-        float x[kApKeep][N], most = 0.0f;
-        auto look = [&](const float (&y)[N]) {
+        const T* src = rows + (int64_t)(q0 + first - kv0) * ld + from0;
+        constexpr int kKeep = sizeof(Group<T, N>) == 32 ? 4 : 8;  // groups a lane keeps
+        Group<T, N> x[kKeep];
+        float most = 0.0f;
+        auto look = [&](const Group<T, N>& from) {
+            float y[N];
+            from.get(y);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float b = __builtin_fabsf(y[e]);
                 if (b < __builtin_huge_valf()) most = fmaxf(most, b);
             }
         };
+        // f(k, row, column) for the passes over `tokens` rows: the first kKeep, then the rest
+        auto next = [&](int& row, int& col) {
+            col += DSPARK_WAVE;
+            if (col >= per) col = 0, row += rows_of;
+        };
+        auto walk = [&](int tokens, auto kept, auto rest) {
+            int row = 0, col = 0;
+            asm("" : "+s"(tokens));  // (the passes' masks are made anew, not held)
 #pragma unroll
-        for (int k = 0; k < kApKeep; ++k) {
-            const int g = k * DSPARK_WAVE + lane;
-            if (g < groups) load_values<T, N>(src + (int64_t)(g / per) * ld + (g % per) * N, x[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kApKeep; ++k)
-            if (k * DSPARK_WAVE + lane < groups) look(x[k]);
-        for (int g = kApKeep * DSPARK_WAVE + lane; g < groups; g += DSPARK_WAVE) {
-            float y[N];
-            load_values<T, N>(src + (int64_t)(g / per) * ld + (g % per) * N, y);
-            look(y);
-        }
+            for (int k = 0; k < kKeep; ++k) {
+                if (row >= tokens) return;
+                if (row + lrow < tokens && col + lcol < per) kept(k, row, col * N);
+                next(row, col);
+            }
+            for (; row < tokens; next(row, col))
+                if (row + lrow < tokens && col + lcol < per) rest(row, col * N);
+        };
+        // (the rows, the page and its scale are loaded together)
+        walk(n, [&](int k, int row, int c) { x[k].load(src + row * ld + c); }, [](int, int) {});
+        if ((unsigned)pid >= (unsigned)a.num_pages) continue;
+        const int slot = lo % a.page;
+        uint8_t* dst = cache + pid * s0 + slot * s2 + to0;
+        float* scale = scales + ((int64_t)pid * a.Hkv + h) * (a.page / a.block) + slot / a.block;
+        const float s_old = first > lo ? *scale : 0.0f;
+        walk(n, [&](int k, int, int) { look(x[k]); },
+             [&](int row, int c) {
+                 Group<T, N> y;
+                 y.load(src + row * ld + c);
+                 look(y);
+             });
         most = wave_max(most);
 
         int e = 0x7fffffff;  // of the scale
@@ -137,30 +176,34 @@ __global__ __launch_bounds__(kApThreads) void cache_append(ApParams p) {
         if (e == 0x7fffffff) e = 0;  // nothing but zeros (or nothing finite)
         const float s = __uint_as_float((uint32_t)(e + 127) << 23), inv = __uint_as_float((uint32_t)(127 - e) << 23);
 
-#pragma unroll
-        for (int k = 0; k < kApKeep; ++k) {
-            const int g = k * DSPARK_WAVE + lane;
-            if (g < groups) store_codes<N>(dst + (int64_t)(first - lo + g / per) * st[2] + (g % per) * N, x[k], inv);
-        }
-        for (int g = kApKeep * DSPARK_WAVE + lane; g < groups; g += DSPARK_WAVE) {
+        uint8_t* to = dst + (first - lo) * s2;
+        auto round = [&](const Group<T, N>& from, int row, int c) {
             float y[N];
-            load_values<T, N>(src + (int64_t)(g / per) * ld + (g % per) * N, y);
-            store_codes<N>(dst + (int64_t)(first - lo + g / per) * st[2] + (g % per) * N, y, inv);
-        }
+            from.get(y);
+            store_codes<N>(to + row * s2 + c, y, inv);
+        };
+        walk(n, [&](int k, int row, int c) { x[k].keep(), round(x[k], row, c); },
+             [&](int row, int c) {
+                 Group<T, N> y;
+                 y.load(src + row * ld + c);
+                 round(y, row, c);
+             });
         if (first > lo && s_old != s) {
             const float ratio = s_old * inv;
-            for (int g = lane; g < (first - lo) * per; g += DSPARK_WAVE) {
-                uint8_t* c = dst + (int64_t)(g / per) * st[2] + (g % per) * N;
+            auto again = [&](int row, int c) {
+                uint8_t* at = dst + row * s2 + c;
                 float y[N];
                 if constexpr (N == 1) {
-                    y[0] = e4m3_to_f32(*c);
+                    y[0] = e4m3_to_f32(*at);
                 } else {
-                    const uint2 w = *(const uint2*)c;
+                    const uint2 w = *(const uint2*)at;
 #pragma unroll
                     for (int b = 0; b < 4; ++b) y[b] = e4m3_to_f32(w.x >> (8 * b)), y[4 + b] = e4m3_to_f32(w.y >> (8 * b));
                 }
-                store_codes<N>(c, y, ratio);
-            }
+                store_codes<N>(at, y, ratio);
+            };
+            for (int row = 0, col = 0; row < first - lo; next(row, col))
+                if (row + lrow < first - lo && col + lcol < per) again(row, col * N);
         }
         if (lane == 0) *scale = s;
     }
@@ -172,14 +215,13 @@ hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
     ApParams p;
     p.a = a;
     p.nblk = (int)(((int64_t)a.max_q - 1) / a.block + 2);
-    p.sides = a.v ? 2 : 1;
-    p.items = (int64_t)a.R * p.nblk * p.sides * a.Hkv;
+    p.head_groups = (a.Hkv + kApWaves - 1) / kApWaves;
     // 8 values at a time where rows and slots allow 16-byte loads and 8-byte stores
     const int64_t per = a.bf16 ? 8 : 4;
     bool wide = (uintptr_t)a.k % 16 == 0 && (uintptr_t)a.v % 16 == 0 && (uintptr_t)a.k_cache % 8 == 0 &&
                 (uintptr_t)a.v_cache % 8 == 0 && a.k_ld % per == 0 && (!a.v || a.v_ld % per == 0);
     for (int i = 0; i < 3; ++i) wide = wide && a.ks[i] % 8 == 0 && (!a.v || a.vs[i] % 8 == 0);
-    const dim3 grid((unsigned)std::min<int64_t>((p.items + kApWaves - 1) / kApWaves, kApGrid));
+    const dim3 grid((unsigned)(p.head_groups * (a.v ? 2 : 1)), (unsigned)a.R, (unsigned)std::min(p.nblk, kApBlocks));
     if (a.bf16 && wide) hipLaunchKernelGGL((cache_append<uint16_t, 8>), grid, dim3(kApThreads), 0, s, p);
     else if (a.bf16) hipLaunchKernelGGL((cache_append<uint16_t, 1>), grid, dim3(kApThreads), 0, s, p);
     else if (wide) hipLaunchKernelGGL((cache_append<float, 8>), grid, dim3(kApThreads), 0, s, p);
