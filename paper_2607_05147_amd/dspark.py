@@ -428,13 +428,14 @@ _CODES = (torch.uint8, torch.float8_e4m3fn)
 
 def _on(stream, *tensors) -> C.c_void_p:
     """The stream's handle; every tensor has to be on its device, the current one."""
+    here = torch.cuda.current_device()
     if stream is None:
-        stream = torch.cuda.current_stream()
+        stream = torch.cuda.current_stream(here)
+    elif stream.device.index != here:
+        raise DSparkError(f"the call's stream is on {stream.device}, the current device is {here}")
     for t in tensors:
-        if t is not None and t.device != stream.device:
-            raise DSparkError(f"a tensor on {t.device}, the call's stream on {stream.device}")
-    if stream.device.index != torch.cuda.current_device():
-        raise DSparkError(f"the call's stream is on {stream.device}, the current device is {torch.cuda.current_device()}")
+        if t is not None and (not isinstance(t, torch.Tensor) or t.get_device() != here):
+            raise DSparkError(f"a tensor on {getattr(t, 'device', None)}, the call's stream on {stream.device}")
     return C.c_void_p(stream.cuda_stream)
 
 
@@ -610,8 +611,8 @@ def _page_state(block_table, kv_len, ref):
     return R, max_pages, ref.shape[0]
 
 
-def _page_call(block_table, kv_len, page_size, ref, bufs, ws, what, stream):
-    """What reserve, fork and compact share: sizes, buffers, workspace and the state's check."""
+def _page_call(block_table, kv_len, page_size, ref, bufs, ws, what, stream, *more):
+    """What reserve, fork and compact share: sizes, buffers, workspace, the stream and the state's check."""
     R, max_pages, num_pages = _page_state(block_table, kv_len, ref)
     if bufs is not None and bufs.num_pages != num_pages:
         raise DSparkError(f"bufs hold {bufs.num_pages} pages, ref {num_pages}")
@@ -620,10 +621,10 @@ def _page_call(block_table, kv_len, page_size, ref, bufs, ws, what, stream):
         _used_on(stream, ws)
     else:
         ws_bytes = ws.numel() * ws.element_size()
-    _on(stream, block_table, kv_len, ref, ws, *([] if bufs is None else bufs.tensors[:1]))
+    on = _on(stream, block_table, kv_len, ref, ws, *more, *([] if bufs is None else bufs.tensors[:1]))
     if debug_checks():
         _debug_raise(check_page_inputs(block_table, kv_len, page_size, ref, stream), what)
-    return R, max_pages, num_pages, ws, ws_bytes
+    return R, max_pages, num_pages, ws, ws_bytes, on
 
 
 def dspark_pages_reserve(block_table: torch.Tensor, kv_len: torch.Tensor, cu_q: torch.Tensor, page_size: int,
@@ -632,8 +633,8 @@ def dspark_pages_reserve(block_table: torch.Tensor, kv_len: torch.Tensor, cu_q: 
     """Pages for cu_q[r+1] - cu_q[r] more tokens of each request; block_table and ref change in place.
     Returns step_len int32 [R], the kv_len of the step (0: not served).  bufs: what is copied where a
     partly filled page is shared (None: nothing)."""
-    R, max_pages, num_pages, ws, ws_bytes = _page_call(block_table, kv_len, page_size, ref, bufs, ws,
-                                                       "dspark_pages_reserve", stream)
+    R, max_pages, num_pages, ws, ws_bytes, on = _page_call(block_table, kv_len, page_size, ref, bufs, ws,
+                                                           "dspark_pages_reserve", stream, cu_q, step_len)
     _dev(cu_q, "cu_q", torch.int32, (R + 1,))
     if step_len is None:
         step_len = torch.empty(R, dtype=torch.int32, device=ref.device)
@@ -641,7 +642,7 @@ def dspark_pages_reserve(block_table: torch.Tensor, kv_len: torch.Tensor, cu_q: 
     _dev(step_len, "step_len", torch.int32, (R,))
     st = lib().dspark_pages_reserve(_p(block_table), max_pages, _p(kv_len), _p(cu_q), R, page_size, _p(ref), num_pages,
                                     None if bufs is None else bufs.array, 0 if bufs is None else len(bufs.tensors),
-                                    _p(step_len), _p(ws), ws_bytes, _on(stream, cu_q, step_len))
+                                    _p(step_len), _p(ws), ws_bytes, on)
     _raise(st, "dspark_pages_reserve")
     return step_len
 
@@ -678,15 +679,15 @@ def dspark_pages_fork(block_table: torch.Tensor, kv_len: torch.Tensor, page_size
                       ws: Optional[torch.Tensor] = None, stream=None) -> None:
     """Requests child [n] (of length 0) share the pages of parent [n], up to len [n] tokens (None: all);
     block_table, kv_len and ref change in place."""
-    R, max_pages, num_pages, ws, ws_bytes = _page_call(block_table, kv_len, page_size, ref, None, ws, "dspark_pages_fork",
-                                                       stream)
+    R, max_pages, num_pages, ws, ws_bytes, on = _page_call(block_table, kv_len, page_size, ref, None, ws,
+                                                           "dspark_pages_fork", stream, parent, child, len)
     _dev(parent, "parent", torch.int32)
     n = parent.numel()
     _dev(parent, "parent", torch.int32, (n,))
     _dev(child, "child", torch.int32, (n,))
     _dev(len, "len", torch.int32, (n,), optional=True)
     st = lib().dspark_pages_fork(_p(block_table), max_pages, _p(kv_len), R, page_size, _p(ref), num_pages, _p(parent),
-                                 _p(child), _p(len), n, _p(ws), ws_bytes, _on(stream, parent, child, len))
+                                 _p(child), _p(len), n, _p(ws), ws_bytes, on)
     _raise(st, "dspark_pages_fork")
 
 
@@ -695,15 +696,15 @@ def dspark_pages_compact(block_table: torch.Tensor, kv_len: torch.Tensor, page_s
                          ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Moves the pages in use to ids 0 .. used - 1; block_table, ref and the buffers change in place.
     Returns used int32 [1] (device)."""
-    R, max_pages, num_pages, ws, ws_bytes = _page_call(block_table, kv_len, page_size, ref, bufs, ws,
-                                                       "dspark_pages_compact", stream)
+    R, max_pages, num_pages, ws, ws_bytes, on = _page_call(block_table, kv_len, page_size, ref, bufs, ws,
+                                                           "dspark_pages_compact", stream, used)
     if used is None:
         used = torch.empty(1, dtype=torch.int32, device=ref.device)
         _used_on(stream, used)
     _dev(used, "used", torch.int32, (1,))
     st = lib().dspark_pages_compact(_p(block_table), max_pages, _p(kv_len), R, page_size, _p(ref), num_pages,
                                     None if bufs is None else bufs.array, 0 if bufs is None else len(bufs.tensors),
-                                    _p(used), _p(ws), ws_bytes, _on(stream, used))
+                                    _p(used), _p(ws), ws_bytes, on)
     _raise(st, "dspark_pages_compact")
     return used
 
