@@ -7,28 +7,36 @@
 // The codes widen to bf16 exactly (one instruction for two), so they enter bf16
 // products as they are, and the scales stay outside: s_k multiplies the fp32 scores
 // (a lane's eight keys lie in one block, so by one value), s_v the fp32
-// probabilities.  bf16 queries enter as they are, fp32 ones as three bf16 terms
-// (24 bits: exact); the probabilities as two terms (to within 2^-17, below the bf16
-// output's 2^-9) or three (2^-24).
+// probabilities.  fp32 queries enter as three bf16 terms (24 bits: exact), and so do
+// their probabilities (2^-24), with the values' codes as bf16.  bf16 queries enter as
+// they are, and their p * s_v rounded once to fp16 (2^-11, a quarter of the bf16
+// output's 2^-9, and the values' codes as fp16): one product where two bf16 terms (2^-17)
+// take two and four more instructions a value; 128 requests 283 us against 373.
+// (The fp8 products of this part add with few bits: 2^-10 of a score's largest product.)
 //
 // Half the cache's bytes of bf16, the same products: bound by HBM, with the widening
-// and the softmax on the vector ALUs next.  The work is cut as in attn_stream.hip: a
-// worker is a single wave with its own K and V buffers in LDS and an equal range of
-// the batch's steps (attn_ranges.h), so nothing in its loop waits for another wave;
-// a wave's row tiles share one widening of the keys and values (waves that shared a
-// buffer would each widen it).
+// and the softmax on the vector ALUs next.  The work is cut as in attn_stream.hip into
+// equal ranges of the batch's steps (attn_ranges.h), the heads of a range on one XCD
+// (token-major pages have them side by side).  A range's worker is
 //
-//   * K and V rows are copied from their page straight into LDS, one step ahead:
-//     64 keys a step (32 at head sizes above 128), 16 of them inside one page.  Rows
-//     are 16 * CH bytes (padded head sizes are filled from a zero block), chunks
-//     XOR-swizzled by the copy so that the operand reads are free of bank conflicts.
-//     A step's scales are one more copy, of a value per 16 keys.
+//   * for few rows a single wave with one K and one V buffer in LDS, refilled as soon as
+//     its operands are in registers: nothing in its loop waits for another wave, and
+//     ten or more workers a CU hide its chain of dependences.  Its two row tiles share
+//     one widening of the keys and values;
+//   * for many rows four waves of one tile that share a ring of three buffers: every
+//     wave copies a part of each step, two steps ahead, and all meet once a step.
+//
+//   * K and V rows are copied from their page straight into LDS, 32 or 64 keys a
+//     step, 16 of them inside one page.  Rows are 16 * CH bytes (padded head sizes are
+//     filled from a zero block), chunks XOR-swizzled by the copy so that the operand
+//     reads are free of bank conflicts.  A step's scales are one more copy, of a value
+//     per 16 keys.
 //   * S^T = K Q^T on v_mfma_f32_16x16x32_bf16: a 16-byte read has 16 dims of a key, two
 //     operand slices (the queries are laid out alike).  The keys of an operand row
 //     are permuted so that the scores already have the B layout of the next product.
 //   * O^T += V^T P^T, V^T by transposing 8-byte reads (eight keys of a dim).
-//   * softmax online in exp2 units, the running maximum moved only when it grows by
-//     more than 2^8 (exact after the final normalisation);
+//   * softmax online in exp2 units relative to a reference that seldom moves (exact
+//     after the final normalisation), below;
 //   * a worker that finds a sum non-finite computes its rows again key by key
 //     (scaled_rows), so that a non-finite value reaches only the rows that see it.
 #include <algorithm>
@@ -52,12 +60,16 @@ typedef __attribute__((address_space(3))) float lds_f32;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-// The running reference of a row's scores moves when one exceeds it by 2^kHead, to kBias
-// below that.  fp32: p is at most 2^8.  bf16 queries, p in fp16: at most 2^15, and full
-// precision down to 2^-21 of the row's largest (fp16 is normal from 2^-14).
+// A row's reference m: its exponents are relative to it.  It moves when one exceeds it by
+// kHead, to kBias below that.  fp32: of the scores, p is at most 2^8.  bf16 queries: of
+// the scores + log2 |s_v|, so that p * s_v, which fp16 holds, is at most 2^15 and of full
+// precision down to 2^-21 of the row's largest (fp16 is normal from 2^-14), whatever the
+// scales are; p alone is fp32 (scales outside 2^-100 .. 2^100 count as those; larger ones
+// overflow, and their rows are computed again).
 template <bool F32> struct Ref {
     static constexpr float kBias = F32 ? 0.0f : 7.0f, kHead = F32 ? 8.0f : 15.0f;
 };
+constexpr float kMaxLog = 100.0f;
 constexpr int kMinUnits = 4;         // steps per wave, at least
 constexpr int kPageRegs = 2;         // page ids per lane: 128 pages of a range at a time
 constexpr int kMaxD = 256;
@@ -274,17 +286,14 @@ struct Tiles {
     u32x4 qf[N][2 * S][TQ];  // queries, B operand: slice 2 i + h holds dims 64 i + 16 lq + 8 h ..
     int lim[N];              // last key that the row sees
     int lim_min;             // of the wave's rows
-    f32x4 acc[N][DB];        // bf16: of v * s_v / vref
-    float m[N], l[N];        // reference of the scores; sum of the probabilities
-    float vref, vinv;        // bf16: a power of two that the values' scales stay below
+    f32x4 acc[N][DB];
+    float m[N], l[N];        // reference; sum of the probabilities
 
     __device__ __forceinline__ void load(const Params& p, int g, int first, int q0, int ql, int kv) {
         const AttnArgs& a = p.a;
         const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
         const int rows = ql * p.group;
         lim_min = 0x7fffffff;
-        vref = 0.0f;
-        vinv = 1.0f;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const int row = first + 16 * W * j + lr;
@@ -326,10 +335,10 @@ struct Tiles {
 
     // Scores of a step's keys (half h: keys key0 + 32 h + 8 lq + 4 mb + e of row lr), and from
     // them the probabilities times the values' scales.  FULL: every row sees every key.
-    // vscale[h]: of the lane's eight keys of the half, and of the other sixteen's block.
+    // kscale, vscale[h]: of the lane's eight keys of the half.
     template <bool FULL>
     __device__ __forceinline__ void scores(const Params& p, const u32x4 (&kf)[H][2][S], const float (&kscale)[H],
-                                           const float (&vscale)[H][2], int key0, int kv, u32x4 (&pb)[H][N][TP]) {
+                                           const float (&vs)[H], int key0, int kv, u32x4 (&pb)[H][N][TP]) {
         const int lq = (here(threadIdx.x) & 63) >> 4;
         f32x4 sc[N][H][2];
 #pragma unroll
@@ -355,18 +364,12 @@ struct Tiles {
         // The eight keys of a lane have one scale, so their maximum is taken before it
         // (where a scale is negative this is the least of them: a reference too low,
         // which at worst overflows and is computed again)
-        float bm[N], ks[H], vs[H], most = 0.0f;
+        float bm[N], ks[H], lv[H];
         bool need = false;
 #pragma unroll
         for (int h = 0; h < H; ++h) {
             ks[h] = kscale[h] * p.scale2;
-            vs[h] = vscale[h][0];
-            if constexpr (!F32)
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const float y = __builtin_fabsf(vscale[h][x]);
-                    if (y < __builtin_huge_valf()) most = fmaxf(most, y);
-                }
+            lv[h] = F32 ? 0.0f : fminf(fmaxf(__builtin_amdgcn_logf(__builtin_fabsf(vs[h])), -kMaxLog), kMaxLog);
         }
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -386,22 +389,13 @@ struct Tiles {
                 b = vmax(vmax(b, x[3]), y[0]);
                 b = vmax(vmax(b, y[1]), y[2]);
                 b = vmax(b, y[3]);
-                if constexpr (FULL) b *= ks[h];
+                b = FULL ? __builtin_fmaf(b, ks[h], lv[h]) : b + lv[h];
                 bm[j] = h ? vmax(bm[j], b) : b;
             }
             bm[j] = row_max4(bm[j]);
             need = need || bm[j] > m[j] + Ref<F32>::kHead;
         }
-        // fp16 holds p * s_v only relative to the largest s_v so far
-        const bool vneed = !F32 && most > vref;
-        if (__builtin_amdgcn_ballot_w64(need || vneed)) {
-            float f = 1.0f;
-            if (vneed) {  // (alike in all lanes)
-                const float up = __uint_as_float(min((__float_as_uint(most) + 0x7fffffu) & 0x7f800000u, 0x7e800000u));
-                f = vref / up;
-                vref = up;
-                vinv = 1.0f / up;
-            }
+        if (__builtin_amdgcn_ballot_w64(need)) {
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const bool up = bm[j] > m[j] + Ref<F32>::kHead;
@@ -409,13 +403,10 @@ struct Tiles {
                 const float alpha = up ? __builtin_amdgcn_exp2f(m[j] - mn) : 1.0f;
                 l[j] *= alpha;
 #pragma unroll
-                for (int d = 0; d < DB; ++d) acc[j][d] *= alpha * f;
+                for (int d = 0; d < DB; ++d) acc[j][d] *= alpha;
                 m[j] = mn;
             }
         }
-        if constexpr (!F32)
-#pragma unroll
-            for (int h = 0; h < H; ++h) vs[h] *= vinv;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const float mu = m[j] == -__builtin_huge_valf() ? 0.0f : m[j];
@@ -488,23 +479,21 @@ struct Tiles {
             }
             const int t = row / p.group;
             const int64_t orow = (int64_t)(q0 + t) * a.Hq + g * p.group + (row - t * p.group);
-            if constexpr (!F32) {
-#pragma unroll
-                for (int d = 0; d < DB; ++d) acc[j][d] *= vref;
-            }
-            const float inv = 1.0f / l[j];
+            float inv = 1.0f / l[j];
+            if (!whole && !(l[j] > 0.0f)) inv = 1.0f;  // (no key of the range is the row's)
             if (whole) {
                 if (a.lse && lq == 0) a.lse[orow] = (m[j] + log2f(l[j])) * kLn2;
             } else if (lq == 0) {
-                part[rr] = m[j];
-                part[C::Rows + rr] = l[j];
+                // (ranges may differ by more in m and in l than fp32's exponent spans)
+                part[rr] = l[j] > 0.0f ? m[j] + log2f(l[j]) : m[j];
+                part[C::Rows + rr] = l[j] > 0.0f ? 1.0f : l[j];
             }
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 const int dim = 16 * d + 4 * lq;  // four consecutive dims of this lane
                 const f32x4 o = acc[j][d];
                 if (!whole) {
-                    *(f32x4*)(part + 2 * C::Rows + (int64_t)rr * C::Dp + dim) = o;
+                    *(f32x4*)(part + 2 * C::Rows + (int64_t)rr * C::Dp + dim) = o * inv;
                 } else if (dim < a.Dv) {
                     if (F32) *(f32x4*)((float*)a.out + orow * a.Dv + dim) = o * inv;
                     else
@@ -533,15 +522,14 @@ struct Reads {
         v = lds0 + C::TileB + t * C::RowB + 16 * v_slot<CH>(t, 0) + 8 * (lr & 1);
         scale = lds0 + 2 * C::TileB + (lq >> 1) * C::ScaleStep;
     }
-    __device__ __forceinline__ void keys(uint32_t buf, int h, u32x4 (&kf)[2][C::S], float& ks, float (&vs)[2]) const {
+    __device__ __forceinline__ void keys(uint32_t buf, int h, u32x4 (&kf)[2][C::S], float& ks, float& vs) const {
 #pragma unroll
         for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
             for (int i = 0; i < C::S; ++i)
                 kf[mb][i] = *lds_ptr<const lds_u32x4>(k[i] + buf + (32 * h + 4 * mb) * C::RowB);
         ks = *lds_ptr<const lds_f32>(scale + buf + 2 * h * C::ScaleStep);
-        vs[0] = *lds_ptr<const lds_f32>(scale + buf + 2 * h * C::ScaleStep + C::ScaleV);
-        vs[1] = *lds_ptr<const lds_f32>(((scale + buf) ^ C::ScaleStep) + 2 * h * C::ScaleStep + C::ScaleV);
+        vs = *lds_ptr<const lds_f32>(scale + buf + 2 * h * C::ScaleStep + C::ScaleV);
     }
     __device__ __forceinline__ void values(uint32_t buf, int h, i32x2 (&vf)[C::DB]) const {
 #pragma unroll
@@ -673,7 +661,7 @@ __device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, con
             const bool more = n + 1 < nseg;
             wait_copies<P * S>();  // K and scales of step n
             u32x4 kf[H][2][S], pb[H][N][C::TP];
-            float ks[H], vs[H][2];
+            float ks[H], vs[H];
             i32x2 vf[H][C::DB];
 #pragma unroll
             for (int h = 0; h < H; ++h) reads.keys(0, h, kf[h], ks[h], vs[h]);
@@ -712,8 +700,7 @@ __device__ __forceinline__ bool attend_shared(const Params& p, const uint32_t ld
     typedef Cfg<F32, CH, W, T> C;
     constexpr int S = C::S, H = C::H, P = C::P, R = C::Ring;
     constexpr int kOps = P * S / W;  // copies of a wave for a step's keys, and for its values
-    static_assert(P * S % W == 0 && (kOps <= S || kOps % S == 0) && S % (kOps < S ? kOps : S) == 0, "a wave's copies");
-    static_assert(kOps <= S, "a wave's copies lie in one piece");
+    static_assert(P * S % W == 0 && kOps <= S && S % kOps == 0, "a wave's copies lie in one piece");
     const AttnArgs& a = p.a;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -800,7 +787,7 @@ __device__ __forceinline__ bool attend_shared(const Params& p, const uint32_t ld
             issue();
             if constexpr (N > 0) {
                 u32x4 kf[H][2][S], pb[H][N][C::TP];
-                float ks[H], vs[H][2];
+                float ks[H], vs[H];
                 i32x2 vf[H][C::DB];
 #pragma unroll
                 for (int h = 0; h < H; ++h) reads.keys(buf, h, kf[h], ks[h], vs[h]);

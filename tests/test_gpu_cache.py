@@ -5,11 +5,13 @@ Tolerances.  Appending is compared exactly: with scales that are powers of two a
 code is one rounding of an exact quotient.  Attention: codes and scales are exact,
 so the error is that of the arithmetic.  bf16: the output's rounding is at most
 2^-8 / 2 per value (half a step of 2^-8 relative, eps / 2 = 2^-9 on the mean of a
-binade's two ends), the probabilities' two bf16 terms add 2^-16 and the fp32 sums less;
-per row in the 2-norm the rounding alone is below 2^-8: 4e-3.  fp32: three bf16 terms are
-exact to 2^-24, a score sums up to 256 products in fp32, 256 * 2^-24 * sum |q k| at worst
-and its square root in practice; with |scores| up to about 8 the probabilities move by
-at most a few 1e-6 relative: 1e-5, the existing fp32 tolerance of this attention.
+binade's two ends), a probability times its value's scale is rounded once to fp16,
+2^-11 of itself or 2^-25, where the row's largest is 2^7 or more: 2^-12 in the mean
+of squares; per row in the 2-norm the output's rounding alone is below 2^-8: 4e-3.
+fp32: three bf16 terms are exact to 2^-24, a score sums up to 256 products in fp32,
+256 * 2^-24 * sum |q k| at worst and its square root in practice; with |scores| up to
+about 8 the probabilities move by at most a few 1e-6 relative: 1e-5, the existing fp32
+tolerance of this attention.
 """
 import numpy as np
 import pytest
@@ -199,10 +201,11 @@ def test_table_entries_outside_the_cache_read_a_page_inside(D, kv):
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("what", ["k", "v", "k_scale", "v_scale", "v_inf"])
-def test_what_is_not_finite_reaches_only_the_rows_that_see_it(dt, what):
+@pytest.mark.parametrize("group,D", [(2, 64), (9, 64), (8, 128), (12, 256), (2, 72)])  # 10 rows; 40 to 60; on the vector ALUs
+def test_what_is_not_finite_reaches_only_the_rows_that_see_it(dt, what, group, D):
     # the last verify token's key, value or scales: earlier rows do not see it
     page = 16
-    c = Case([5, 5], [320 + 5, 33], 4, 2, 64, 64, page, 16, dt, seed=6)
+    c = Case([5, 5], [320 + 5, 33], 2 * group, 2, D, D, page, 16, dt, seed=6)
     c.kv[1] = 33
     j = int(c.kv[0]) - 1
     pg, sl = c.table[0, j // page], j % page
@@ -219,9 +222,9 @@ def test_what_is_not_finite_reaches_only_the_rows_that_see_it(dt, what):
     out, _ = attend(c, c.on_device(), q)
     bad = ~torch.isfinite(out.float()).all(2).cpu().numpy()  # [rows, heads]
     rows = [int(c.cu[0]) + t for t in sees]
-    assert bad[rows][:, :2].all()
+    assert bad[rows][:, :group].all()
     rest = np.ones_like(bad)
-    rest[np.ix_(rows, [0, 1])] = False
+    rest[np.ix_(rows, range(group))] = False
     assert not bad[rest].any()
     same = out.float().cpu().numpy()[rest] - good.float().cpu().numpy()[rest]
     assert np.abs(same).max() <= 2e-2 * np.abs(good.float().cpu().numpy()).max()
@@ -254,7 +257,7 @@ def test_scales_that_are_no_powers_of_two():
 def test_references_that_keep_moving(D, group, dt):
     # scores and values that grow from block to block, by up to 2^30 each: the running
     # maximum and the values' reference move at every block, inside a step too
-    c = Case([3, 1], [600, 250], 2 * group, 2, D, D, 16, 16, dt, seed=22)
+    c = Case([9, 1], [600, 250], 2 * group, 2, D, D, 16, 16, dt, seed=22)
     for r in range(c.R):
         n = -(-int(c.kv[r]) // 16)
         for i in range(n):
@@ -266,7 +269,7 @@ def test_references_that_keep_moving(D, group, dt):
 
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("group", [1, 4])
+@pytest.mark.parametrize("group", [1, 4, 24])
 @pytest.mark.parametrize("what", [float("inf"), 2.0 ** 100, float("nan")])
 def test_scales_of_blocks_without_tokens_may_be_anything(what, group, dt):
     # page 0 too, which stands in for table entries past a context
@@ -280,6 +283,62 @@ def test_scales_of_blocks_without_tokens_may_be_anything(what, group, dt):
                     c.scale[n][pg, :, b] = what
     out, lse = attend(c, c.on_device(), q)
     check_attention(c, q, out, lse)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("group,D", [(2, 64), (9, 64), (4, 128), (8, 128), (12, 256)])
+@pytest.mark.parametrize("ratio", [20, 40])
+def test_large_values_that_the_scores_leave_out(ratio, group, D, dt):
+    # the first 64 keys score far below the rest and their values' scales are 2^ratio larger:
+    # what counts is the product of both (2^-18 and less of the others' here)
+    c = Case([5, 1], [400, 90], 2 * group, 2, D, D, 16, 16, dt, seed=24)
+    low = (ratio + 18) * np.log(2.0)
+    q = (0.5 + torch.from_numpy(c.rng.random((c.rows, c.Hq, D), dtype=np.float32))).to(dt).to(dev())
+    for r in range(c.R):
+        for i in range(-(-int(c.kv[r]) // 16)):
+            at = c.table[r, i]
+            # (the others' scores lie around 2, those of the first near -low)
+            mean = 4.0 if i >= 4 else -2.0 * low
+            x = np.clip(c.rng.normal(64, 8, (2, 16, D)), 0, 128) * np.sign(mean)
+            c.code["k"][at] = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+            c.scale["k"][at] = np.float32(abs(mean) / (64 * D * D ** -0.5))
+            if i < 4:
+                c.scale["v"][at] = 2.0 ** (ratio - 6)
+    out, lse = attend(c, c.on_device(), q)
+    check_attention(c, q, out, lse)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("group", [2, 8])
+@pytest.mark.parametrize("exps", [(-100,), (-60,), (60,), (110,), (-100, 60), (-3, 90)])
+def test_values_scales_of_any_size(exps, group, dt):
+    # block by block in turn; the second request's keys and scales are small enough for one range
+    c = Case([5, 2], [3000, 130], 2 * group, 2, 128, 128, 64, 16, dt, seed=25)
+    for r in range(c.R):
+        for b in range(-(-int(c.kv[r]) // 16)):
+            c.scale["v"][c.table[r, b // 4], :, b % 4] = 2.0 ** exps[b % len(exps)]
+    q = queries(c)
+    out, lse = attend(c, c.on_device(), q)
+    check_attention(c, q, out, lse)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("group", [2, 8])
+def test_negative_scales_and_scales_of_zero(group, dt):
+    c = Case([5, 2], [700, 130], 2 * group, 2, 128, 128, 64, 16, dt, seed=26)
+    for n in ("k", "v"):
+        c.scale[n] *= c.rng.choice(np.array([-1.0, 1.0, 1.0, 0.0], np.float32), c.scale[n].shape)
+    q = queries(c)
+    out, lse = attend(c, c.on_device(), q)
+    check_attention(c, q, out, lse)
+
+
+def test_values_that_are_all_zero():
+    for group in (2, 8):
+        c = Case([5, 2], [700, 130], 2 * group, 2, 128, 128, 64, 16, torch.bfloat16, seed=27)
+        c.scale["v"][:] = 0.0
+        out, lse = attend(c, c.on_device(), queries(c))
+        assert bool((out == 0).all()) and bool(torch.isfinite(lse).all())
 
 
 def test_values_that_alias_the_keys():
@@ -487,8 +546,9 @@ def test_offsets_past_32_bits():
 
 # ------------------------------------------------------------------ graphs, streams, refusals
 
-def test_append_and_attention_in_a_graph():
-    c = Case([3, 1, 4], [300, 1000, 64], 16, 2, 128, 128, 64, 64, torch.bfloat16, seed=18)
+@pytest.mark.parametrize("group", [8, 16])  # one wave a range; four
+def test_append_and_attention_in_a_graph(group):
+    c = Case([3, 1, 4], [300, 1000, 64], 2 * group, 2, 128, 128, 64, 64, torch.bfloat16, seed=18)
     x, q, d = fill(c, torch.bfloat16), queries(c), c.on_device()
     need = dspark.dspark_verify_attn_scaled_workspace_size(c.R, c.max_q, c.Hq, c.Hkv, 128, 128, d["table"].shape[1], c.page, c.block, c.dt)
     ws = torch.empty(need, dtype=torch.uint8, device=dev())
@@ -526,6 +586,23 @@ def test_another_stream():
     s.wait_stream(torch.cuda.current_stream())
     out, lse = attend(c, d, q, stream=s)
     assert torch.equal(out, want)
+
+
+def test_two_calls_at_once():
+    # each with its own workspace and outputs, over one cache
+    c = Case([3, 1, 9], [3000, 90, 5000], 32, 2, 128, 128, 64, 64, torch.bfloat16, seed=28)
+    d, q = c.on_device(), queries(c)
+    want, lse = attend(c, d, q)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        got = []
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got.append(dspark.dspark_verify_attn_scaled(q, d["kc"], d["vc"], c.strides["k"], c.strides["v"], d["ks"], d["vs"], c.block, d["table"],
+                                                            d["kv"], d["cu"], c.max_q, c.Dv, c.page, c.Dqk ** -0.5, want_lse=True))
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) and torch.equal(x, lse) for o, x in got)
 
 
 def test_refusals():
