@@ -127,6 +127,10 @@ def _raise(st: int, what: str) -> None:
 
 
 def _dev(t: Optional[torch.Tensor], name: str, dtype=None, shape=None, optional=False):
+    # (a step's host time is mostly these checks: what passes takes one line)
+    if (isinstance(t, torch.Tensor) and t.is_cuda and (dtype is None or t.dtype == dtype) and
+            (shape is None or t.shape == shape) and t.is_contiguous()):
+        return t
     if t is None:
         if optional:
             return None
@@ -143,7 +147,7 @@ def _dev(t: Optional[torch.Tensor], name: str, dtype=None, shape=None, optional=
 
 
 def _p(t: Optional[torch.Tensor]):
-    return None if t is None else C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream) -> C.c_void_p:
@@ -259,7 +263,8 @@ def check_page_inputs(block_table: torch.Tensor, kv_len: torch.Tensor, page_size
 def _cache_pages(cache: torch.Tensor, strides: Sequence[int], heads: int, page_size: int, dim: int) -> int:
     """Pages a flat cache holds: page p is readable when its last element,
     p * s0 + (heads - 1) * s1 + (page_size - 1) * s2 + dim - 1, is inside."""
-    s0, s1, s2 = (int(x) for x in strides)
+    s0, s1, s2 = strides
+    s0, s1, s2 = int(s0), int(s1), int(s2)
     span = (heads - 1) * s1 + (page_size - 1) * s2 + dim
     return max(0, (cache.numel() - span) // s0 + 1) if s0 > 0 else 0
 
@@ -426,17 +431,16 @@ def dspark_verify_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
 _CODES = (torch.uint8, torch.float8_e4m3fn)
 
 
-def _on(stream, *tensors) -> C.c_void_p:
+def _on(stream, *tensors) -> int:
     """The stream's handle; every tensor has to be on its device, the current one."""
     here = torch.cuda.current_device()
-    if stream is None:
-        stream = torch.cuda.current_stream(here)
-    elif stream.device.index != here:
+    if stream is not None and stream.device.index != here:
         raise DSparkError(f"the call's stream is on {stream.device}, the current device is {here}")
     for t in tensors:
         if t is not None and (not isinstance(t, torch.Tensor) or t.get_device() != here):
-            raise DSparkError(f"a tensor on {getattr(t, 'device', None)}, the call's stream on {stream.device}")
-    return C.c_void_p(stream.cuda_stream)
+            raise DSparkError(f"a tensor on {getattr(t, 'device', None)}, the call's stream on device {here}")
+    # (the handle alone: an object for the current stream takes longer than a launch)
+    return torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
 
 
 def _used_on(stream, *tensors) -> None:
@@ -474,8 +478,11 @@ def _scaled_cache(k_cache, v_cache, k_strides, v_strides, k_scale, v_scale, bloc
     return R, max_pages, num_pages, Hkv
 
 
+_Strides3 = C.c_int64 * 3
+
+
 def _strides3(st):
-    return (C.c_int64 * 3)(*[int(x) for x in st])
+    return _Strides3(*map(int, st))
 
 
 def _new_rows(t, name, dtype, Hkv):
@@ -514,7 +521,7 @@ def dspark_cache_append(k: torch.Tensor, v: Optional[torch.Tensor], k_cache: tor
     if debug_checks():
         _debug_raise(check_verify_inputs(block_table, kv_len, cu_q, max_q, page_size, num_pages, stream),
                      "dspark_cache_append")
-    st = lib().dspark_cache_append(C.c_void_p(k.data_ptr()), None if v is None else C.c_void_p(v.data_ptr()), k_ld, v_ld,
+    st = lib().dspark_cache_append(_p(k), _p(v), k_ld, v_ld,
                                    _DT[k.dtype], _p(k_cache), _p(v_cache), _strides3(k_strides),
                                    None if v is None else _strides3(v_strides), _p(k_scale), _p(v_scale), block,
                                    _p(block_table), max_pages, num_pages, _p(kv_len), _p(cu_q), R, max_q, Hkv, Dqk, Dv,
