@@ -271,11 +271,13 @@ dspark_status dspark_verify_attn(const void* q, const void* k_cache, const void*
  * fp32).  Table entries outside [0, num_pages) read the nearest page inside.
  * v_cache may alias k_cache, with v_scale = k_scale.  Which kernels run:
  *   - head sizes up to 256, cache strides multiples of 16 bytes (page stride
- *     below 2^31, token stride below 2^24), q, k_cache and v_cache 16-byte and
- *     out 8-byte (bf16) or 16-byte (fp32) aligned, Dqk and Dv multiples of 16:
- *     matrix cores, the codes widened to bf16 (exact), bf16 queries as they are,
- *     fp32 queries as three bf16 terms (exact), probabilities as two (bf16) or
- *     three (fp32) bf16 terms; HBM-bound;
+ *     below 2^31, token stride below 2^24, page_size * token stride below 2^31),
+ *     q, k_cache and v_cache 16-byte and out 8-byte (bf16) or 16-byte (fp32)
+ *     aligned, Dqk and Dv multiples of 16, page_size below 2^20 and fewer than
+ *     2^32 scales: matrix cores, HBM-bound.  The codes are widened exactly.  bf16
+ *     queries enter as they are, a probability times its value's scale rounded
+ *     once to fp16 (2^-11; products below 2^-21 of a row's largest lose bits);
+ *     fp32 queries and probabilities as three bf16 terms (2^-24);
  *   - anything else: vector ALUs.
  *   ws of dspark_verify_attn_scaled_workspace_size bytes, 256-aligned; a smaller
  *   one is refused (DSPARK_EWORKSPACE).  A non-finite key, value or scale
