@@ -885,7 +885,6 @@ static auto with_cfg(bool bf16, int ch, int w, int t, F f) {
         if (w == 4) DS_CFG(true, 8, 4, 1);
         DS_CFG(true, 8, 1, 1);
     }
-    if (w == 4) DS_CFG(true, 16, 4, 1);
     DS_CFG(true, 16, 1, 1);
 #undef DS_CFG
 }
@@ -898,14 +897,23 @@ static Geom geom(const AttnArgs& a) {
     const int64_t max_kv = (int64_t)a.max_pages * a.page;
     g.direct = max_kv <= kDirectKeys && (rows + 15) / 16 <= kDirectChunks;
     // One wave takes up to 16 rows, or 32 in two tiles; above, four waves share the keys and
-    // values.  (us, 8 KV heads, contexts of 1000-3000 keys, one wave / four: 32 rows of
-    // heads of 64 145 / 168, of 128 142 / 147, of 256 188 / 141, fp32 112 / 116, 107 / 110 and
-    // 109 / 149; 48 rows 315 / 183, 205 / 157, 259 / 154, fp32 164 / 143, 147 / 131 and
-    // 150 / 157.  Two tiles a wave of four, 128 requests of 64/8 heads: 136 rows each 650
-    // against 780, but 324 against 283 where a request has 35 on average.)  Short
-    // contexts are bound by a wave's own chain of steps: one wave, one tile.
-    const int alone = g.ch == 16 ? (a.bf16 ? 16 : 48) : 32;
-    g.w = g.direct || rows <= alone ? 1 : 4;
+    // values.  What is known here is the most rows that a request may have; a schedule
+    // gives most of them a quarter of it, and fewer tiles than waves leave waves idle, which
+    // fp32, whose tiles take three times the products, feels most.  us, 48 requests of
+    // 2000-4000 keys, 8 KV heads, four waves / one (fp32 heads of 256: always one):
+    //    rows (at most)    8 (68)    20 (68)   36 (68)   68 (68)   16 (136)  40 (136)  136 (136)
+    //    bf16, 64          39 / 39   50 / 45   55 / 62   90 / 90   47 / 43   56 / 59   129 / 140
+    //    bf16, 128         72 / 68   78 / 78   84 / 101 136 / 159  76 / 73   86 / 100  198 / 254
+    //    bf16, 256        126 / 129 138 / 172 148 / 257 247 / 453 135 / 149 151 / 271  369 / 792
+    //    fp32, 64          47 / 47   67 / 62   75 / 90  127 / 141  60 / 61   77 / 87   184 / 225
+    //    fp32, 128        103 / 71  110 / 94  116 / 143 203 / 244 109 / 80  121 / 148  304 / 428
+    //    fp32, 256        270 / 130 279 / 178 292 / 258 534 / 464 274 / 149 292 / 267  804 / 800
+    // 32 of at most 32 rows, another batch: bf16 168 / 145, 147 / 142 and 141 / 188.
+    // Two tiles a wave of four, 128 requests of 64/8 heads: 136 rows each 650 against
+    // 780, but 324 against 283 where a request has 35 on average.  Short contexts are
+    // bound by a wave's own chain of steps: one wave, one tile.
+    const int alone = a.bf16 ? (g.ch == 16 ? 16 : 32) : g.ch == 4 ? 32 : 80;
+    g.w = g.direct || rows <= alone || (!a.bf16 && g.ch == 16) ? 1 : 4;
     g.t = g.w == 1 && !g.direct && rows > 16 && (a.bf16 ? g.ch <= 8 : g.ch == 4) ? 2 : 1;
     g.rc_max = (int)((rows + 16 * g.w * g.t - 1) / (16 * g.w * g.t));
     const int64_t items = (int64_t)a.R * a.Hkv * g.rc_max;
