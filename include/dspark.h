@@ -319,7 +319,7 @@ dspark_status dspark_verify_attn_scaled(const void* q, const void* k_cache, cons
  *               buffer is the page_bytes bytes at base + p * page_stride (base
  *               device memory; keys, values, scales, layer by layer).  The array
  *               is read during the call only.  At most 1024, page_stride at most
-               2^31; n_bufs 0 copies nothing.
+ *               2^31; n_bufs 0 copies nothing.
  *   ws          dspark_pages_workspace_size(R, num_pages) bytes, 256-aligned.
  *
  * dspark_pages_reserve: pages for cu_q[r+1] - cu_q[r] more tokens of every
