@@ -149,7 +149,8 @@ def test_compact_edges():
         b.compact()
 
 
-@pytest.mark.parametrize("sizes", [(16384 * 3 + 16, 64), (1, 2, 3, 5, 20), (16,) * 70])
+@pytest.mark.parametrize("sizes", [(16384 * 3 + 16, 64), (1, 2, 3, 5, 20), (16,) * 70, (512, 516, 511, 16384, 8, 528, 513),
+                                   tuple(1024 + 16 * i if i % 3 else 12 + i for i in range(130))], ids=range(5))
 def test_copies_of_every_size(sizes):
     b = Both([5, 0, 70, 3], 16, 40, 8, seed=7, sizes=sizes)
     b.fork([0], [1])
