@@ -115,12 +115,18 @@ __device__ __forceinline__ bool range_find(const Ranges& p, int w, int total_row
 // block b to XCD b % 8 as the device deals them, so that what the heads share of a page's
 // lines is fetched into one L2.
 constexpr int kXcds = 8;
-template <int STEP, bool XCD = false, typename F>
+//
+// GROUP: a workgroup's waves are workers of their own, consecutive ones.
+template <int STEP, bool XCD = false, int GROUP = 1, typename F>
 __device__ __forceinline__ void range_walk(const Ranges& p, F f) {
     const AttnArgs& a = p.a;
     const int total_rows = range_total_rows(a);
+    const int wave = GROUP > 1 ? (int)__builtin_amdgcn_readfirstlane(threadIdx.x / DSPARK_WAVE) : 0;
+    const int first = GROUP > 1 ? threadIdx.x % DSPARK_WAVE : threadIdx.x;
     if (p.direct) {
-        const int rc = blockIdx.y, g = blockIdx.x % a.Hkv, r = blockIdx.x / a.Hkv;
+        const int item = blockIdx.x * GROUP + wave;
+        const int rc = blockIdx.y, g = item % a.Hkv, r = item / a.Hkv;
+        if (GROUP > 1 && r >= a.R) return;
         int q0, ql, kv;
         if (!range_shape(a, r, total_rows, q0, ql, kv) || rc * p.chunk_rows >= ql * p.group) return;
         const int ns = (kv + STEP - 1) / STEP;
@@ -128,9 +134,9 @@ __device__ __forceinline__ void range_walk(const Ranges& p, F f) {
         return;
     }
     const int heads = p.by_head ? 1 : a.Hkv;  // of this worker's list
-    int worker = blockIdx.x;
+    int worker = blockIdx.x * GROUP + wave;  // (those past the last have an empty range)
     if (XCD && p.by_head) {
-        const int i = blockIdx.x / kXcds;
+        const int i = blockIdx.x / kXcds * GROUP + wave;
         worker = (i / a.Hkv * kXcds + blockIdx.x % kXcds) * a.Hkv + i % a.Hkv;
     }
     int64_t u0, u1, ur;
@@ -143,7 +149,7 @@ __device__ __forceinline__ void range_walk(const Ranges& p, F f) {
         const int ns = (kv + STEP - 1) / STEP;
         const int nrc = (ql * p.group + p.chunk_rows - 1) / p.chunk_rows;
         const int units = ok ? heads * nrc * ns : 0;
-        if (ok && threadIdx.x == 0) p.head[32 + r] = ur;
+        if (ok && first == 0) p.head[32 + r] = ur;
         int local = (int)(u - ur);
         while (local < units && u < u1) {
             const int item = local / ns;

@@ -73,6 +73,7 @@ constexpr float kMaxLog = 100.0f;
 constexpr int kMinUnits = 4;         // steps per wave, at least
 constexpr int kPageRegs = 2;         // page ids per lane: 128 pages of a range at a time
 constexpr int kMaxD = 256;
+constexpr int kGroup = 4;            // single-wave workers of a workgroup
 
 // CH: 16-byte chunks of an LDS row: head sizes up to 16 * CH.  W: waves of a worker;
 // T: 16-row tiles of a wave.
@@ -93,7 +94,8 @@ struct Cfg {
     static constexpr int ScaleStep = W == 1 ? 4 : 256 * W / P, ScaleV = W == 1 ? 4 * P : 4;
     static constexpr int BufB = 2 * TileB + 256 * W;          // K, V, scales
     static constexpr int Ring = W == 1 ? 1 : 3;  // buffers
-    static constexpr int LdsB = Ring * BufB;
+    static constexpr int LdsB = Ring * BufB;                  // of a worker
+    static constexpr int Group = W == 1 ? kGroup : 1;         // workers of a workgroup
     static constexpr int LdsFit = 160 * 1024 / LdsB;          // workers of a CU, by LDS
     // registers: accumulators, queries, scores and probabilities of the row tiles; operands
     static constexpr int Regs = T * (4 * DB + 8 * S * TQ + 8 * (W == 1 ? H : 1) * (TP > 2 ? TP + 1 : 2)) + 8 * (W == 1 ? H : 1) * S + 84;
@@ -548,7 +550,7 @@ __device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, con
     typedef Cfg<F32, CH, 1, T> C;
     constexpr int S = C::S, H = C::H, P = C::P;
     const AttnArgs& a = p.a;
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x & 63;
     const int row0 = rc * C::Rows;
     Tiles<F32, CH, 1, T, N> tiles;
     tiles.load(p, g, row0, q0, ql, kv);
@@ -818,15 +820,16 @@ __device__ __forceinline__ bool attend_shared(const Params& p, const uint32_t ld
 }
 
 template <bool F32, int CH, int W, int T>
-__global__ __launch_bounds__(DSPARK_WAVE * W) __attribute__((amdgpu_waves_per_eu(Cfg<F32, CH, W, T>::Eu)))
+__global__ __launch_bounds__(DSPARK_WAVE * (W == 1 ? kGroup : W)) __attribute__((amdgpu_waves_per_eu(Cfg<F32, CH, W, T>::Eu)))
 void attn_scaled_kernel(Params p) {
     typedef Cfg<F32, CH, W, T> C;
-    __shared__ __align__(256) unsigned char lds[C::LdsB];
+    __shared__ __align__(256) unsigned char lds[C::LdsB * C::Group];
     uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0];
+    if (C::Group > 1) lds0 += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * C::LdsB;
     asm volatile("" : "+s"(lds0));
     const int wave = place<W>(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
     bool again = false;
-    range_walk<C::Step, true>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
+    range_walk<C::Step, true, C::Group>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
         // (a body for each number of tiles: tests of it would cut the step into pieces that
         // the compiler cannot interleave)
         const int n = (ql * p.group - rc * C::Rows + 15) / 16;  // tiles, of all waves
@@ -844,7 +847,7 @@ void attn_scaled_kernel(Params p) {
     // (a walk of its own, so that the step loop above holds none of its registers; a wave
     // goes over its own rows only)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what the lanes wrote above comes before what others write below
-    range_walk<C::Step, true>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
+    range_walk<C::Step, true, C::Group>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
         scaled_rows<F32, CH, W, T>(p, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
     });
 }
@@ -990,8 +993,12 @@ hipError_t launch_attn_scaled(const AttnArgs& a, const CacheScales& c, void* ws,
         constexpr bool F = decltype(f32)::value;
         constexpr int CH = decltype(ch)::value, W = decltype(w)::value, T = decltype(t)::value;
         typedef scaled::Cfg<F, CH, W, T> C;
-        const dim3 grid = g.direct ? dim3((unsigned)(a.R * a.Hkv), (unsigned)g.rc_max) : dim3((unsigned)g.workers);
-        hipLaunchKernelGGL((scaled::attn_scaled_kernel<F, CH, W, T>), grid, dim3(DSPARK_WAVE * W), 0, s, p);
+        // (the workers of an XCD fill its workgroups)
+        const int64_t lists = g.by_head ? kXcds : 1;
+        auto groups = [](int64_t n) { return (n + C::Group - 1) / C::Group; };
+        const dim3 grid = g.direct ? dim3((unsigned)groups((int64_t)a.R * a.Hkv), (unsigned)g.rc_max)
+                                   : dim3((unsigned)(lists * groups(g.workers / lists)));
+        hipLaunchKernelGGL((scaled::attn_scaled_kernel<F, CH, W, T>), grid, dim3(DSPARK_WAVE * W * C::Group), 0, s, p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || g.direct) return e;
         return launch_merge<F, C::Rows, C::Dp, C::Step>(p, s);
