@@ -98,7 +98,8 @@ struct Cfg {
     static constexpr int Group = W == 1 ? kGroup : 1;         // workers of a workgroup
     static constexpr int LdsFit = 160 * 1024 / LdsB;          // workers of a CU, by LDS
     // registers: accumulators, queries, scores and probabilities of the row tiles; operands
-    static constexpr int Regs = T * (4 * DB + 8 * S * TQ + 8 * (W == 1 ? H : 1) * (TP > 2 ? TP + 1 : 2)) + 8 * (W == 1 ? H : 1) * S + 84;
+    static constexpr int Hr = W == 1 ? H : 1;  // (halves at a time)
+    static constexpr int Regs = T * (4 * DB + 8 * S * TQ + Hr * (8 + 4 * TP)) + 8 * Hr * S + 80;
     static constexpr int RegFit = (Regs <= 128 ? 16 : Regs <= 168 ? 12 : Regs <= 256 ? 8 : 4) / W;
     static constexpr int Cu = LdsFit < RegFit ? LdsFit : RegFit;  // workers of a CU
     static constexpr int Eu = Cu * W >= 16 ? 4 : Cu * W >= 12 ? 3 : Cu * W >= 8 ? 2 : 1;  // waves of a SIMD
@@ -905,12 +906,13 @@ static Geom geom(const AttnArgs& a) {
     // fp32, whose tiles take three times the products, feels most.  us, 48 requests of
     // 2000-4000 keys, 8 KV heads, four waves / one (fp32 heads of 256: always one):
     //    rows (at most)    8 (68)    20 (68)   36 (68)   68 (68)   16 (136)  40 (136)  136 (136)
-    //    bf16, 64          39 / 39   50 / 45   55 / 62   90 / 90   47 / 43   56 / 59   129 / 140
-    //    bf16, 128         72 / 68   78 / 78   84 / 101 136 / 159  76 / 73   86 / 100  198 / 254
-    //    bf16, 256        126 / 129 138 / 172 148 / 257 247 / 453 135 / 149 151 / 271  369 / 792
-    //    fp32, 64          47 / 47   67 / 62   75 / 90  127 / 141  60 / 61   77 / 87   184 / 225
-    //    fp32, 128        103 / 71  110 / 94  116 / 143 203 / 244 109 / 80  121 / 148  304 / 428
-    //    fp32, 256        270 / 130 279 / 178 292 / 258 534 / 464 274 / 149 292 / 267  804 / 800
+    //    bf16, 64          41 / 38   48 / 44   56 / 60   86 / 87   45 / 42   56 / 58   126 / 136
+    //    bf16, 128         71 / 67   78 / 77   85 / 100 135 / 159  75 / 73   85 / 98   196 / 248
+    //    bf16, 256        128 / 128 140 / 168 148 / 256 245 / 456 134 / 146 153 / 266  376 / 787
+    //    fp32, 64          48 / 41   66 / 56   77 / 78  126 / 115  60 / 50   76 / 77   185 / 181
+    //    fp32, 128        100 / 70  109 / 91  118 / 140 208 / 238 109 / 79  121 / 147  317 / 418
+    //    fp32, 256        270 / 127 279 / 176 292 / 263 534 / 462 274 / 147 292 / 272  804 / 793
+    // (8 requests of 500-1000 keys, fp32, 64: four 1.5 to 6 us the shorter.)
     // 32 of at most 32 rows, another batch: bf16 168 / 145, 147 / 142 and 141 / 188.
     // Two tiles a wave of four, 128 requests of 64/8 heads: 136 rows each 650 against
     // 780, but 324 against 283 where a request has 35 on average.  Short contexts are
