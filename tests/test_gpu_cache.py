@@ -341,6 +341,20 @@ def test_values_that_are_all_zero():
         assert bool((out == 0).all()) and bool(torch.isfinite(lse).all())
 
 
+@pytest.mark.parametrize("page,tail", [(16, 1), (64, 700)])  # contexts of a few steps; cut into ranges
+def test_as_many_requests_as_there_may_be(page, tail):
+    rng = np.random.default_rng(29)
+    kv = rng.integers(1, 30, 8192)
+    kv[-1] = tail
+    c = Case([1] * 8192, kv, 4, 2, 64, 64, page, 16, torch.bfloat16, seed=29)
+    x, q, d = fill(c, torch.bfloat16), queries(c), c.on_device()
+    out, lse = attend(c, d, q)
+    check_attention(c, q, out, lse, requests=[0, 1, 63, 64, 4095, 8190, 8191])
+    want = expected(c, x)
+    append(c, d, x)
+    check_append(c, d, want)
+
+
 def test_values_that_alias_the_keys():
     c = Case([3, 2], [130, 50], 8, 1, 128, 96, 32, 32, torch.bfloat16, seed=9)
     c.code["v"], c.scale["v"] = c.code["k"][..., :96], c.scale["k"]

@@ -73,7 +73,7 @@ class Both:
         assert int(used) == want
 
 
-@pytest.mark.parametrize("R,page,num_pages", [(1, 16, 12), (5, 16, 60), (70, 32, 1100), (300, 16, 5000), (1500, 16, 12000)])
+@pytest.mark.parametrize("R,page,num_pages", [(1, 16, 12), (5, 16, 60), (70, 32, 1100), (300, 16, 5000), (1500, 16, 12000), (8192, 16, 40000)])
 def test_a_life_of_steps(R, page, num_pages):
     rng = np.random.default_rng(R)
     most = min(num_pages // (2 * R) + 3, 40) * page
