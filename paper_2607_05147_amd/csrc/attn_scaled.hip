@@ -42,8 +42,9 @@
 //   * O^T += V^T P^T, V^T by transposing 8-byte reads (eight keys of a dim).
 //   * softmax online in exp2 units relative to a reference that seldom moves (exact
 //     after the final normalisation), below;
-//   * a worker that finds a sum non-finite computes its rows again key by key
-//     (scaled_rows), so that a non-finite value reaches only the rows that see it.
+//   * a worker that finds a sum non-finite, or too low for the rounding of what it adds up,
+//     computes its rows again key by key (scaled_rows), so that a non-finite value reaches
+//     only the rows that see it.  Slow: 16 ms where one of 128 requests has such rows.
 #include <algorithm>
 #include <type_traits>
 
@@ -68,13 +69,20 @@ constexpr float kLn2 = 0.6931471805599453f;
 // A row's reference m: its exponents are relative to it.  It moves when one exceeds it by
 // kHead, to kBias below that.  fp32: of the scores, p is at most 2^8.  bf16 queries: of
 // the scores + log2 |s_v|, so that p * s_v, which fp16 holds, is at most 2^15 and of full
-// precision down to 2^-21 of the row's largest (fp16 is normal from 2^-14), whatever the
-// scales are; p alone is fp32 (scales outside 2^-100 .. 2^100 count as those; larger ones
-// overflow, and their rows are computed again).
+// precision down to 2^-21 of the row's largest (fp16 is normal from 2^-14); p alone is
+// fp32 (scales outside 2^-100 .. 2^100 count as those; larger ones overflow, and their rows
+// are computed again).
 template <bool F32> struct Ref {
     static constexpr float kBias = F32 ? 0.0f : 7.0f, kHead = F32 ? 8.0f : 15.0f;
 };
 constexpr float kMaxLog = 100.0f;
+// Where the largest p * s_v goes with values near zero, what counts may be what fp16 rounds
+// to multiples of 2^-24: an error of at most 2^-25 a key, times a code of at most 448.  A
+// row whose largest sum is below kLeast for every key of its range, where that error could
+// exceed 2^-9 of it, is computed again.  (A key with p * s_v of 2^7 and a code of 1 in any
+// dim is enough for 18000 keys.)
+constexpr float kLeast = 448.0f / (1 << 16);
+constexpr int kNotFinite = 1, kLow = 2;  // why rows are computed again
 constexpr int kMinUnits = 4;         // steps per wave, at least
 constexpr int kPageRegs = 2;         // page ids per lane: 128 pages of a range at a time
 constexpr int kMaxD = 256;
@@ -209,14 +217,16 @@ __device__ __forceinline__ int place(int wave) {
     return W == 1 ? 0 : (wave + 2 * (int)(blockIdx.x / kRangeCUs)) % W;
 }
 
-// The rows of a chunk over the same steps key by key on the vector ALUs, where the
-// products came out non-finite: a product over 16 rows and 32 keys also multiplies the
-// keys that a row does not see, by a probability of 0, and 0 times a non-finite value
-// is NaN.  Every row takes only its own keys here, as the vector-ALU kernels do.
+// The rows of a chunk over the same steps key by key on the vector ALUs, in fp32, where the
+// products came out non-finite or too low for their roundings: a product over 16 rows and
+// 32 keys also multiplies the keys that a row does not see, by a probability of 0, and 0
+// times a non-finite value is NaN.  Every row takes only its own keys here, as the
+// vector-ALU kernels do.  `why`: if only kLow, values that are all zeros need nothing (a
+// cache that was never filled takes a look at its values, not this).
 template <bool F32, int CH, int W, int T>
 __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const int g, const int rc, const int q0,
                                             const int ql, const int kv, const int s0, const int s1, const int ns,
-                                            const int64_t slot) {
+                                            const int64_t slot, const int why) {
     typedef Cfg<F32, CH, W, T> C;
     typedef typename std::conditional<F32, float, uint16_t>::type E;
     constexpr int kPer = (C::Dp + DSPARK_WAVE - 1) / DSPARK_WAVE;  // value dims per lane
@@ -233,6 +243,19 @@ __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const 
     const uint8_t* vc = (const uint8_t*)a.v + gv * p.vs1;
     const bool whole = s0 + z == 0 && s1 == ns;
     float* part = p.part + (slot + z) * ((int64_t)C::Rows * (C::Dp + 2));
+    if (!F32 && !(why & kNotFinite)) {
+        const int end = min(kv, s1 * C::Step);
+        bool some = false;
+        for (int k0 = (s0 + z) * C::Step; k0 < end && !some; k0 += DSPARK_WAVE) {
+            const int key = min(k0 + lane, end - 1), at = key % page;
+            const int64_t pg = clamp_page(p, bt[key / page]);
+            const u32x4* vr = (const u32x4*)(vc + pg * p.vs0 + (int64_t)at * p.vs2);
+            uint32_t bits = 0;
+            for (int d = 0; d < a.Dv / 16 + z; ++d) bits |= (vr[d][0] | vr[d][1] | vr[d][2] | vr[d][3]) & 0x7f7f7f7fu;
+            some = __builtin_amdgcn_ballot_w64(bits && p.cs.v[(pg * a.Hkv + gv) * p.nb + at / p.cs.block] != 0.0f) != 0;
+        }
+        if (!some) return;
+    }
     for (int rr = 0; rr < nrows; ++rr) {
         if (W > 1 && (rr >> 4) % W != place<W>(wave)) continue;  // the wave's own tiles
         const int row = row0 + rr, t = row / group;
@@ -245,10 +268,16 @@ __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const 
             const int key = min(k0 + lane, end - 1), at = key % page;
             const int64_t pg = clamp_page(p, bt[key / page]);
             const uint8_t* kr = kc + pg * p.ks0 + (int64_t)at * p.ks2;
+            const uint64_t vr = (uint64_t)(uintptr_t)vc + pg * p.vs0 + (int64_t)at * p.vs2;
             const int64_t si = (pg * a.Hkv + gv) * p.nb + at / p.cs.block;
             float sc = 0.0f;
-            for (int d = 0; d < a.Dqk + z; ++d)
-                sc += Elem<E>::load((const E*)a.q, orow * a.Dqk + d) * e4m3_to_f32(kr[d]);
+            for (int d = 0; d < a.Dqk + z; d += 16) {  // (rows are 16-byte aligned, as for the copies)
+                const u32x4 kk = *(const u32x4*)(kr + d);
+                E qq[16];
+                __builtin_memcpy(qq, __builtin_assume_aligned((const E*)a.q + orow * a.Dqk + d, 16), sizeof(qq));
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc += Elem<E>::load(qq, e) * e4m3_to_f32(kk[e >> 2] >> (8 * (e & 3)));
+            }
             sc *= p.cs.k[si] * p.scale2;
             if (k0 + lane >= end) sc = -__builtin_huge_valf();
             const float mn = fmaxf(m, wave_max(sc));
@@ -256,17 +285,25 @@ __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const 
             float pr = sc == -__builtin_huge_valf() ? 0.0f : exp2f(sc - (mn == -__builtin_huge_valf() ? 0.0f : mn));
             l = l * alpha + wave_sum(pr);
             m = mn;
-            pr *= p.cs.v[si];
+            pr = k0 + lane < end ? pr * p.cs.v[si] : 0.0f;
 #pragma unroll
             for (int e = 0; e < kPer; ++e) o[e] *= alpha;
-            for (int j = 0; j < min(DSPARK_WAVE, end - k0); ++j) {
-                const int64_t pj = clamp_page(p, bt[(k0 + j) / page]);
-                const uint8_t* vr = vc + pj * p.vs0 + (int64_t)((k0 + j) % page) * p.vs2;
-                const float w = __shfl(pr, j, DSPARK_WAVE);
+            // (past the end the last key again, 0 times; eight keys at a time hide their loads)
+            const int nj = min(DSPARK_WAVE, end - k0);
+            for (int j0 = 0; j0 < nj; j0 += 8) {
+                uint8_t code[8][kPer];
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) {
-                    const int d = lane + e * DSPARK_WAVE;
-                    if (d < a.Dv) o[e] += w * e4m3_to_f32(vr[d]);
+                for (int j = 0; j < 8; ++j) {
+                    const uint8_t* from = (const uint8_t*)(uintptr_t)(
+                        (uint64_t)(uint32_t)__shfl((int)vr, j0 + j, DSPARK_WAVE) | (uint64_t)(uint32_t)__shfl((int)(vr >> 32), j0 + j, DSPARK_WAVE) << 32);
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) code[j][e] = lane + e * DSPARK_WAVE < a.Dv ? from[lane + e * DSPARK_WAVE] : 0;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float w = __shfl(pr, j0 + j, DSPARK_WAVE);
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) o[e] += w * e4m3_to_f32(code[j][e]);
                 }
             }
         }
@@ -465,26 +502,32 @@ struct Tiles {
         }
     }
 
-    // The rows' results, or their partials.  Returns whether a sum of them is not finite
-    // (what is written is then not yet the result).
-    __device__ __forceinline__ bool finish(const Params& p, int g, int row0, int first, int q0, int ql, bool whole,
-                                           float* part) {
+    // The rows' results, or their partials, over `keys` keys.  Returns why they have to be
+    // computed again, if so (what is written is then not yet the result).
+    __device__ __forceinline__ int finish(const Params& p, int g, int row0, int first, int q0, int ql, bool whole,
+                                          float* part, int keys) {
         const AttnArgs& a = p.a;
         const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
-        float big[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // largest sum by magnitude (NaN if one is), in independent chains
+        const float least = kLeast * (float)keys;
+        float most = 0.0f;  // largest sum by magnitude (NaN if one is)
+        bool low = false;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             // total l over the four lanes of a row
             l[j] += __shfl_xor(l[j], 16, 64);
             l[j] += __shfl_xor(l[j], 32, 64);
-            const int row = first + 16 * W * j + lr, rr = row - row0;
-            if (row >= ql * p.group) continue;
-            big[0] = vmax(big[0], l[j]);
+            float big[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // of the row's, in independent chains
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 big[d & 3] = vmax(vmax(__builtin_fabsf(acc[j][d][0]), __builtin_fabsf(acc[j][d][1])), big[d & 3]);
                 big[d & 3] = vmax(vmax(__builtin_fabsf(acc[j][d][2]), __builtin_fabsf(acc[j][d][3])), big[d & 3]);
             }
+            big[0] = vmax(vmax(big[0], big[1]), vmax(big[2], big[3]));
+            if constexpr (!F32) big[1] = row_max4(big[0]);
+            const int row = first + 16 * W * j + lr, rr = row - row0;
+            if (row >= ql * p.group) continue;
+            most = vmax(vmax(big[0], l[j]), most);
+            if constexpr (!F32) low = low || (l[j] > 0.0f && big[1] < least);
             const int t = row / p.group;
             const int64_t orow = (int64_t)(q0 + t) * a.Hq + g * p.group + (row - t * p.group);
             float inv = 1.0f / l[j];
@@ -510,7 +553,8 @@ struct Tiles {
                 }
             }
         }
-        return __builtin_amdgcn_ballot_w64(!(vmax(vmax(big[0], big[1]), vmax(big[2], big[3])) < __builtin_huge_valf())) != 0;
+        return (__builtin_amdgcn_ballot_w64(!(most < __builtin_huge_valf())) ? kNotFinite : 0) |
+               (__builtin_amdgcn_ballot_w64(low) ? kLow : 0);
     }
 };
 
@@ -550,9 +594,9 @@ struct Reads {
 // Steps [s0, s1) of the ns steps of one (request, head, chunk) of N row tiles, by a single
 // wave.  `slot`: where the partial goes when they are not all of them.
 template <bool F32, int CH, int T, int N>
-__device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
-                                       const int q0, const int ql, const int kv, const int s0, const int s1,
-                                       const int ns, const int64_t slot) {
+__device__ __forceinline__ int attend(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
+                                      const int q0, const int ql, const int kv, const int s0, const int s1,
+                                      const int ns, const int64_t slot) {
     typedef Cfg<F32, CH, 1, T> C;
     constexpr int S = C::S, H = C::H, P = C::P;
     const AttnArgs& a = p.a;
@@ -695,16 +739,17 @@ __device__ __forceinline__ bool attend(const Params& p, const uint32_t lds0, con
         for (; n < nseg; ++n) step(n, std::false_type{});
         sb = se;
     }
-    return tiles.finish(p, g, row0, row0, q0, ql, s0 == 0 && s1 == ns, p.part + slot * ((int64_t)C::Rows * (C::Dp + 2)));
+    return tiles.finish(p, g, row0, row0, q0, ql, s0 == 0 && s1 == ns, p.part + slot * ((int64_t)C::Rows * (C::Dp + 2)),
+                        (s1 - s0) * C::Step);
 }
 
 // The same by W waves that share the keys and values, N row tiles in this one (maybe
 // none).  Each wave copies its part of a step, Ring - 1 steps ahead, into a ring of
 // buffers; one barrier a step.
 template <bool F32, int CH, int W, int T, int N>
-__device__ __forceinline__ bool attend_shared(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
-                                              const int q0, const int ql, const int kv, const int s0, const int s1,
-                                              const int ns, const int64_t slot) {
+__device__ __forceinline__ int attend_shared(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
+                                             const int q0, const int ql, const int kv, const int s0, const int s1,
+                                             const int ns, const int64_t slot) {
     typedef Cfg<F32, CH, W, T> C;
     constexpr int S = C::S, H = C::H, P = C::P, R = C::Ring;
     constexpr int kOps = P * S / W;  // copies of a wave for a step's keys, and for its values
@@ -821,8 +866,8 @@ __device__ __forceinline__ bool attend_shared(const Params& p, const uint32_t ld
     }
     if constexpr (N > 0)
         return tiles.finish(p, g, row0, first, q0, ql, s0 == 0 && s1 == ns,
-                            p.part + slot * ((int64_t)C::Rows * (C::Dp + 2)));
-    return false;
+                            p.part + slot * ((int64_t)C::Rows * (C::Dp + 2)), (s1 - s0) * C::Step);
+    return 0;
 }
 
 template <bool F32, int CH, int W, int T>
@@ -834,7 +879,7 @@ void attn_scaled_kernel(Params p) {
     if (C::Group > 1) lds0 += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * C::LdsB;
     asm volatile("" : "+s"(lds0));
     const int wave = place<W>(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
-    bool again = false;
+    int again = 0;
     range_walk<C::Step, true, C::Group>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
         // (a body for each number of tiles: tests of it would cut the step into pieces that
         // the compiler cannot interleave)
@@ -854,7 +899,7 @@ void attn_scaled_kernel(Params p) {
     // goes over its own rows only)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what the lanes wrote above comes before what others write below
     range_walk<C::Step, true, C::Group>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
-        scaled_rows<F32, CH, W, T>(p, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
+        scaled_rows<F32, CH, W, T>(p, r, g, rc, q0, ql, kv, s0, s1, ns, slot, again);
     });
 }
 
