@@ -5,8 +5,9 @@ dtype/shape/contiguity, passes raw pointers to ``libdspark.so`` and raises
 ``DSparkError`` with the library's message when a call fails.  Outputs that are
 not supplied are allocated with torch (device memory plumbing); all
 computation happens in the library's HIP kernels, enqueued on the current
-torch stream unless ``stream`` is given.  There is no fallback: without the
-built library every call raises.
+torch stream unless ``stream`` is given, whose memory the outputs and workspaces that
+a call allocates then are.  There is no fallback: without the built library every
+call raises.
 """
 from __future__ import annotations
 
@@ -156,11 +157,23 @@ def _stream(stream) -> C.c_void_p:
     return C.c_void_p(stream.cuda_stream)
 
 
-def _workspace(nbytes: int, device, ws: Optional[torch.Tensor]) -> Tuple[Optional[torch.Tensor], int]:
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """What a call allocates is memory of the stream that it runs on: of the current stream's, the
+    allocator may give a block that kernels still to come there use, and another stream does not wait
+    for them.  The caller may read it on the current stream too, once that waits for the call's."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
+def _workspace(nbytes: int, device, ws: Optional[torch.Tensor], stream) -> Tuple[Optional[torch.Tensor], int]:
     if nbytes == 0:
         return ws, 0 if ws is None else ws.numel() * ws.element_size()
     if ws is None:
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        ws = _empty(nbytes, torch.uint8, device, stream)
     return ws, ws.numel() * ws.element_size()
 
 
@@ -208,7 +221,7 @@ def check_verify_inputs(block_table: torch.Tensor, kv_len: torch.Tensor, cu_q: t
     R, max_pages = block_table.shape
     _dev(kv_len, "kv_len", torch.int32, (R,))
     _dev(cu_q, "cu_q", torch.int32, (R + 1,))
-    report = torch.empty(4, dtype=torch.int32, device=cu_q.device)
+    report = _empty(4, torch.int32, cu_q.device, stream)
     st = lib().dspark_check_verify_inputs(_p(block_table), max_pages, _p(kv_len), _p(cu_q), R, max_q,
                                           page_size, num_pages, _p(report), _stream(stream))
     _raise(st, "dspark_check_verify_inputs")
@@ -219,7 +232,7 @@ def check_accept_inputs(cu_q: torch.Tensor, u: Optional[torch.Tensor], K: int, s
     _dev(cu_q, "cu_q", torch.int32)
     R = cu_q.numel() - 1
     _dev(u, "u", torch.float32, (R, K + 1), optional=True)
-    report = torch.empty(4, dtype=torch.int32, device=cu_q.device)
+    report = _empty(4, torch.int32, cu_q.device, stream)
     st = lib().dspark_check_accept_inputs(_p(cu_q), _p(u), R, K, _p(report), _stream(stream))
     _raise(st, "dspark_check_accept_inputs")
     return _report(report, "accept", stream)
@@ -228,7 +241,7 @@ def check_accept_inputs(cu_q: torch.Tensor, u: Optional[torch.Tensor], K: int, s
 def check_schedule_inputs(conf: torch.Tensor, stream=None) -> Optional[tuple]:
     _dev(conf, "conf", torch.float32)
     R, K = conf.shape
-    report = torch.empty(4, dtype=torch.int32, device=conf.device)
+    report = _empty(4, torch.int32, conf.device, stream)
     st = lib().dspark_check_schedule_inputs(_p(conf), R, K, _p(report), _stream(stream))
     _raise(st, "dspark_check_schedule_inputs")
     return _report(report, "schedule", stream)
@@ -242,7 +255,7 @@ def check_draft_inputs(u: torch.Tensor, sts_temp: Optional[torch.Tensor] = None,
     _dev(u, "u", torch.float32)
     R, K = u.shape
     _dev(sts_temp, "sts_temp", torch.float32, (K,), optional=True)
-    report = torch.empty(4, dtype=torch.int32, device=u.device)
+    report = _empty(4, torch.int32, u.device, stream)
     st = lib().dspark_check_draft_inputs(_p(u), _p(sts_temp), R, K, _p(report), _stream(stream))
     _raise(st, "dspark_check_draft_inputs")
     return _report(report, "draft", stream)
@@ -253,7 +266,7 @@ def check_page_inputs(block_table: torch.Tensor, kv_len: torch.Tensor, page_size
     """First broken rule of the dspark_pages_* state as (code, request, index,
     value, rule) or None; waits for the check."""
     R, max_pages, num_pages = _page_state(block_table, kv_len, ref)
-    report = torch.empty(4, dtype=torch.int32, device=ref.device)
+    report = _empty(4, torch.int32, ref.device, stream)
     st = lib().dspark_check_page_inputs(_p(block_table), max_pages, _p(kv_len), R, page_size, _p(ref), num_pages,
                                         _p(report), _stream(stream))
     _raise(st, "dspark_check_page_inputs")
@@ -288,15 +301,15 @@ def dspark_schedule(conf: torch.Tensor, sps: torch.Tensor, mode: int = 0,
     _dev(sps, "sps", torch.float64)
     dev = conf.device
     if len_out is None:
-        len_out = torch.empty(R, dtype=torch.int32, device=dev)
+        len_out = _empty(R, torch.int32, dev, stream)
     if cu_q is None:
-        cu_q = torch.empty(R + 1, dtype=torch.int32, device=dev)
+        cu_q = _empty(R + 1, torch.int32, dev, stream)
     if tok_req is None and want_tok_req:
-        tok_req = torch.empty(R * (K + 1), dtype=torch.int32, device=dev)
+        tok_req = _empty(R * (K + 1), torch.int32, dev, stream)
     _dev(len_out, "len", torch.int32, (R,))
     _dev(cu_q, "cu_q", torch.int32, (R + 1,))
     _dev(tok_req, "tok_req", torch.int32, (R * (K + 1),), optional=True)
-    ws, ws_bytes = _workspace(dspark_schedule_workspace_size(R, K), dev, ws)
+    ws, ws_bytes = _workspace(dspark_schedule_workspace_size(R, K), dev, ws, stream)
     if debug_checks() and K > 0:
         _debug_raise(check_schedule_inputs(conf, stream), "dspark_schedule")
     st = lib().dspark_schedule(_p(conf), R, K, _p(sps), sps.numel(), mode, _p(len_out), _p(cu_q),
@@ -335,9 +348,9 @@ def dspark_schedule_capacity(conf_prev: torch.Tensor, sps: torch.Tensor,
     _dev(sps, "sps", torch.float64)
     dev = conf_prev.device
     if capacity is None:
-        capacity = torch.empty(1, dtype=torch.int32, device=dev)
+        capacity = _empty(1, torch.int32, dev, stream)
     _dev(capacity, "capacity", torch.int32, (1,))
-    ws, ws_bytes = _workspace(dspark_schedule_workspace_size(R, K), dev, ws)
+    ws, ws_bytes = _workspace(dspark_schedule_workspace_size(R, K), dev, ws, stream)
     st = lib().dspark_schedule_capacity(_p(conf_prev), R, K, _p(sps), sps.numel(), _p(capacity),
                                         _p(ws), ws_bytes, _stream(stream))
     _raise(st, "dspark_schedule_capacity")
@@ -357,15 +370,15 @@ def dspark_schedule_topk(conf: torch.Tensor, capacity: torch.Tensor,
     _dev(capacity, "capacity", torch.int32, (1,))
     dev = conf.device
     if len_out is None:
-        len_out = torch.empty(R, dtype=torch.int32, device=dev)
+        len_out = _empty(R, torch.int32, dev, stream)
     if cu_q is None:
-        cu_q = torch.empty(R + 1, dtype=torch.int32, device=dev)
+        cu_q = _empty(R + 1, torch.int32, dev, stream)
     if tok_req is None and want_tok_req:
-        tok_req = torch.empty(R * (K + 1), dtype=torch.int32, device=dev)
+        tok_req = _empty(R * (K + 1), torch.int32, dev, stream)
     _dev(len_out, "len", torch.int32, (R,))
     _dev(cu_q, "cu_q", torch.int32, (R + 1,))
     _dev(tok_req, "tok_req", torch.int32, (R * (K + 1),), optional=True)
-    ws, ws_bytes = _workspace(dspark_schedule_workspace_size(R, K), dev, ws)
+    ws, ws_bytes = _workspace(dspark_schedule_workspace_size(R, K), dev, ws, stream)
     st = lib().dspark_schedule_topk(_p(conf), R, K, _p(capacity), _p(len_out), _p(cu_q),
                                     _p(tok_req), _p(ws), ws_bytes, _stream(stream))
     _raise(st, "dspark_schedule_topk")
@@ -403,14 +416,14 @@ def dspark_verify_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
     _dev(kv_len, "kv_len", torch.int32, (R,))
     _dev(cu_q, "cu_q", torch.int32, (R + 1,))
     if out is None:
-        out = torch.empty((rows, Hq, Dv), dtype=q.dtype, device=q.device)
+        out = _empty((rows, Hq, Dv), q.dtype, q.device, stream)
     _dev(out, "out", q.dtype, (rows, Hq, Dv))
     if lse is None and want_lse:
-        lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
+        lse = _empty((rows, Hq), torch.float32, q.device, stream)
     _dev(lse, "lse", torch.float32, (rows, Hq), optional=True)
     need = dspark_verify_attn_workspace_size(R, max_q, Hq, Hkv, Dqk, Dv, max_pages, page_size,
                                              q.dtype)
-    ws, ws_bytes = _workspace(need, q.device, ws)
+    ws, ws_bytes = _workspace(need, q.device, ws, stream)
     if debug_checks():
         num_pages = min(_cache_pages(k_cache, k_strides, Hkv, page_size, Dqk),
                         _cache_pages(v_cache, v_strides, Hkv, page_size, Dv))
@@ -441,14 +454,6 @@ def _on(stream, *tensors) -> int:
             raise DSparkError(f"a tensor on {getattr(t, 'device', None)}, the call's stream on device {here}")
     # (the handle alone: an object for the current stream takes longer than a launch)
     return torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
-
-
-def _used_on(stream, *tensors) -> None:
-    """Tensors that a call allocated itself, where it runs on another stream than the current one."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
 
 
 def _scaled_cache(k_cache, v_cache, k_strides, v_strides, k_scale, v_scale, block, block_table, kv_len, cu_q, page_size,
@@ -550,17 +555,14 @@ def dspark_verify_attn_scaled(q: torch.Tensor, k_cache: torch.Tensor, v_cache: t
     R, max_pages, num_pages, Hkv = _scaled_cache(k_cache, v_cache, k_strides, v_strides, k_scale, v_scale, block,
                                                  block_table, kv_len, cu_q, page_size, Dqk, Dv)
     if out is None:
-        out = torch.empty((rows, Hq, Dv), dtype=q.dtype, device=q.device)
-        _used_on(stream, out)
+        out = _empty((rows, Hq, Dv), q.dtype, q.device, stream)
     _dev(out, "out", q.dtype, (rows, Hq, Dv))
     if lse is None and want_lse:
-        lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
-        _used_on(stream, lse)
+        lse = _empty((rows, Hq), torch.float32, q.device, stream)
     _dev(lse, "lse", torch.float32, (rows, Hq), optional=True)
     if ws is None:
         need = dspark_verify_attn_scaled_workspace_size(R, max_q, Hq, Hkv, Dqk, Dv, max_pages, page_size, block, q.dtype)
-        ws, ws_bytes = _workspace(need, q.device, None)
-        _used_on(stream, ws)
+        ws, ws_bytes = _workspace(need, q.device, None, stream)
     else:
         ws_bytes = ws.numel() * ws.element_size()
     on = _on(stream, q, k_cache, v_cache, k_scale, v_scale, block_table, kv_len, cu_q, out, lse, ws)
@@ -624,8 +626,7 @@ def _page_call(block_table, kv_len, page_size, ref, bufs, ws, what, stream, *mor
     if bufs is not None and bufs.num_pages != num_pages:
         raise DSparkError(f"bufs hold {bufs.num_pages} pages, ref {num_pages}")
     if ws is None:
-        ws, ws_bytes = _workspace(dspark_pages_workspace_size(R, num_pages), ref.device, None)
-        _used_on(stream, ws)
+        ws, ws_bytes = _workspace(dspark_pages_workspace_size(R, num_pages), ref.device, None, stream)
     else:
         ws_bytes = ws.numel() * ws.element_size()
     on = _on(stream, block_table, kv_len, ref, ws, *more, *([] if bufs is None else bufs.tensors[:1]))
@@ -644,8 +645,7 @@ def dspark_pages_reserve(block_table: torch.Tensor, kv_len: torch.Tensor, cu_q: 
                                                            "dspark_pages_reserve", stream, cu_q, step_len)
     _dev(cu_q, "cu_q", torch.int32, (R + 1,))
     if step_len is None:
-        step_len = torch.empty(R, dtype=torch.int32, device=ref.device)
-        _used_on(stream, step_len)
+        step_len = _empty(R, torch.int32, ref.device, stream)
     _dev(step_len, "step_len", torch.int32, (R,))
     st = lib().dspark_pages_reserve(_p(block_table), max_pages, _p(kv_len), _p(cu_q), R, page_size, _p(ref), num_pages,
                                     None if bufs is None else bufs.array, 0 if bufs is None else len(bufs.tensors),
@@ -706,8 +706,7 @@ def dspark_pages_compact(block_table: torch.Tensor, kv_len: torch.Tensor, page_s
     R, max_pages, num_pages, ws, ws_bytes, on = _page_call(block_table, kv_len, page_size, ref, bufs, ws,
                                                            "dspark_pages_compact", stream, used)
     if used is None:
-        used = torch.empty(1, dtype=torch.int32, device=ref.device)
-        _used_on(stream, used)
+        used = _empty(1, torch.int32, ref.device, stream)
     _dev(used, "used", torch.int32, (1,))
     st = lib().dspark_pages_compact(_p(block_table), max_pages, _p(kv_len), R, page_size, _p(ref), num_pages,
                                     None if bufs is None else bufs.array, 0 if bufs is None else len(bufs.tensors),
@@ -745,16 +744,16 @@ def dspark_accept(draft_tok: torch.Tensor, logits: torch.Tensor, cu_q: torch.Ten
     _dev(u, "u", torch.float32, (R, K + 1), optional=True)
     dev = draft_tok.device
     if accepted_len is None:
-        accepted_len = torch.empty(R, dtype=torch.int32, device=dev)
+        accepted_len = _empty(R, torch.int32, dev, stream)
     if next_tok is None:
-        next_tok = torch.empty(R, dtype=torch.int32, device=dev)
+        next_tok = _empty(R, torch.int32, dev, stream)
     if accept_rate is None and want_rate:
-        accept_rate = torch.empty(R * (K + 1), dtype=torch.float32, device=dev)
+        accept_rate = _empty(R * (K + 1), torch.float32, dev, stream)
     _dev(accepted_len, "accepted_len", torch.int32, (R,))
     _dev(next_tok, "next_tok", torch.int32, (R,))
     _dev(accept_rate, "accept_rate", torch.float32, optional=True)
     need = dspark_accept_workspace_size(R, K, V)
-    ws, ws_bytes = _workspace(need, dev, ws)
+    ws, ws_bytes = _workspace(need, dev, ws, stream)
     if debug_checks():
         _debug_raise(check_accept_inputs(cu_q, u, K, stream), "dspark_accept")
     st = lib().dspark_accept(_p(draft_tok), _p(draft_p), C.c_void_p(logits.data_ptr()),
@@ -800,18 +799,18 @@ def dspark_markov_draft(anchor: torch.Tensor, base_logits: torch.Tensor, W1: tor
     _dev(u, "u", torch.float32, (R, K))
     dev = anchor.device
     if draft_tok is None:
-        draft_tok = torch.empty((R, K), dtype=torch.int32, device=dev)
+        draft_tok = _empty((R, K), torch.int32, dev, stream)
     if draft_p is None:
-        draft_p = torch.empty((R, K, V), dtype=torch.float32, device=dev)
+        draft_p = _empty((R, K, V), torch.float32, dev, stream)
     if conf is None:
-        conf = torch.empty((R, K), dtype=torch.float32, device=dev)
+        conf = _empty((R, K), torch.float32, dev, stream)
     _dev(draft_tok, "draft_tok", torch.int32, (R, K))
     _dev(draft_p, "draft_p", torch.float32, (R, K, V))
     _dev(conf, "conf", torch.float32, (R, K))
     need = dspark_markov_draft_workspace_size(R, K, V, rank)
     if need == 0:
         raise DSparkError(f"unsupported shape: R={R} V={V} rank={rank}")
-    ws, ws_bytes = _workspace(need, dev, ws)
+    ws, ws_bytes = _workspace(need, dev, ws, stream)
     if debug_checks():
         _debug_raise(check_draft_inputs(u, sts_temp, stream), "dspark_markov_draft")
     st = lib().dspark_markov_draft(_p(anchor), C.c_void_p(base_logits.data_ptr()),
@@ -858,18 +857,18 @@ def dspark_rnn_draft(anchor: torch.Tensor, base_logits: torch.Tensor, W1: torch.
     _dev(u, "u", torch.float32, (R, K))
     dev = anchor.device
     if draft_tok is None:
-        draft_tok = torch.empty((R, K), dtype=torch.int32, device=dev)
+        draft_tok = _empty((R, K), torch.int32, dev, stream)
     if draft_p is None:
-        draft_p = torch.empty((R, K, V), dtype=torch.float32, device=dev)
+        draft_p = _empty((R, K, V), torch.float32, dev, stream)
     if conf is None:
-        conf = torch.empty((R, K), dtype=torch.float32, device=dev)
+        conf = _empty((R, K), torch.float32, dev, stream)
     _dev(draft_tok, "draft_tok", torch.int32, (R, K))
     _dev(draft_p, "draft_p", torch.float32, (R, K, V))
     _dev(conf, "conf", torch.float32, (R, K))
     need = dspark_rnn_draft_workspace_size(R, K, V, rank)
     if need == 0:
         raise DSparkError(f"unsupported shape: R={R} V={V} rank={rank}")
-    ws, ws_bytes = _workspace(need, dev, ws)
+    ws, ws_bytes = _workspace(need, dev, ws, stream)
     if debug_checks():
         _debug_raise(check_draft_inputs(u, sts_temp, stream), "dspark_rnn_draft")
     st = lib().dspark_rnn_draft(_p(anchor), C.c_void_p(base_logits.data_ptr()),
