@@ -173,13 +173,18 @@ __device__ __forceinline__ void range_walk(const Ranges& p, F f) {
 // Combines the partials of every chunk whose steps several ranges share, in
 // key order.  Workgroups (request and head, part of the rows); a thread takes
 // four values of a row; up to kMergeBatch partials are in flight.  A chain of
-// dependent loads, so the rows are spread over up to kMergeParts workgroups,
-// as long as there are about kMergeGrid (4 requests x 8 heads of up to 136 rows, 32
-// parts against 8: 40.5 and 42.6 us with the attention; 128 requests, 4 and 8: 272 and 273).
+// dependent loads, so the rows are spread over kMergeLeast workgroups, up to
+// kMergeParts where that makes kMergeGrid.  us with the attention, 8 heads, 32 parts
+// against 8: 4 requests of up to 136 rows, 8-bit cache 40.5 and 42.6, bf16 heads of 128
+// 35.9 and 38.6, fp32 107 and 112; but 8 requests of up to 520 rows, fp32 heads of 64,
+// 33.1 and 29.7 (16 parts 29.6), 16 requests 42.0 and 39.2: with more of its workgroups
+// the next call's attention is the slower one.  Fewer than 8 gain nothing (128 requests
+// 272 and 273, 1024 and 2048 the same).
 constexpr int kMergeThreads = 256;
 constexpr int kMergeBatch = 8;
+constexpr int kMergeLeast = 8;
 constexpr int kMergeParts = 32;
-constexpr int kMergeGrid = 4096;
+constexpr int kMergeGrid = 1024;
 template <bool F32, int ROWS, int DP, int STEP>
 __global__ __launch_bounds__(kMergeThreads) void attn_merge(Ranges p) {
     typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -246,7 +251,7 @@ template <bool F32, int ROWS, int DP, int STEP>
 static hipError_t launch_merge(const Ranges& p, hipStream_t s) {
     const int64_t quads = (int64_t)p.a.max_q * p.group * (p.a.Dv / 4);  // of a (request, head), at most
     const int64_t need = quads / kMergeThreads + (quads % kMergeThreads != 0), pairs = (int64_t)p.a.R * p.a.Hkv;
-    const int64_t most = kMergeGrid / pairs < 2 ? 2 : kMergeGrid / pairs < kMergeParts ? kMergeGrid / pairs : kMergeParts;
+    const int64_t most = kMergeGrid / pairs < kMergeLeast ? kMergeLeast : kMergeGrid / pairs < kMergeParts ? kMergeGrid / pairs : kMergeParts;
     hipLaunchKernelGGL((attn_merge<F32, ROWS, DP, STEP>), dim3((unsigned)pairs, (unsigned)(need < most ? need : most)),
                        dim3(kMergeThreads), 0, s, p);
     return hipGetLastError();
