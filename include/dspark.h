@@ -342,7 +342,11 @@ dspark_status dspark_verify_attn_scaled(const void* q, const void* k_cache, cons
  *   its q_len_r tokens (within [0, q_len_r]; accepted_len NULL: all of them):
  *   kv_len_r = step_len_r - q_len_r + kept, and the pages past it are given
  *   back.  Requests with step_len_r outside [1, max_pages * page_size] or q_len_r
- *   outside [0, step_len_r] are left as they are.
+ *   outside [0, step_len_r] are left as they are.  From its reserve to its commit
+ *   a request holds the pages of step_len_r: a step_len is committed once, and the
+ *   other calls of this part (another reserve, trim, compact, a fork to it) come
+ *   before the reserve or after the commit.  Else pages are given back twice, or
+ *   lost: dspark_check_page_inputs with step_len as kv_len looks for that.
  * dspark_pages_trim: kv_len_r = min(kv_len_r, max(new_len_r, 0)), and the pages
  *   past it are given back; new_len_r = 0 ends the request.  A page cut inside
  *   stays shared with its other holders; reserve copies it.

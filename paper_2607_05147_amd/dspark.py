@@ -662,9 +662,11 @@ def dspark_pages_commit(block_table: torch.Tensor, kv_len: torch.Tensor, step_le
     _dev(step_len, "step_len", torch.int32, (R,))
     _dev(cu_q, "cu_q", torch.int32, (R + 1,))
     _dev(accepted_len, "accepted_len", torch.int32, (R,), optional=True)
+    on = _on(stream, block_table, kv_len, step_len, cu_q, accepted_len, ref)
+    if debug_checks():  # (of the lengths that the step has, whose pages are given back)
+        _debug_raise(check_page_inputs(block_table, step_len, page_size, ref, stream), "dspark_pages_commit")
     st = lib().dspark_pages_commit(_p(block_table), max_pages, _p(kv_len), _p(step_len), _p(cu_q), _p(accepted_len), R,
-                                   page_size, _p(ref), num_pages,
-                                   _on(stream, block_table, kv_len, step_len, cu_q, accepted_len, ref))
+                                   page_size, _p(ref), num_pages, on)
     _raise(st, "dspark_pages_commit")
 
 
