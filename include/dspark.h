@@ -566,7 +566,9 @@ dspark_status dspark_rnn_draft(const int32_t* anchor, const void* base_logits,
  * dspark_check_page_inputs (the state of dspark_pages_*): code 1 kv_len_r
  * outside [0, max_pages*page_size] (value kv_len_r); 2 a table entry that
  * request r holds outside [0, num_pages) (index: logical page, value: the
- * entry); 3 one that names a page with ref below 1 (likewise).
+ * entry); 3 one that names a page with ref below 1 (likewise); 4, where no request
+ * breaks the others, one that names a page with ref below the number of held
+ * entries that name it (likewise; the first request that holds such a page).
  * ---------------------------------------------------------------------- */
 dspark_status dspark_check_verify_inputs(const int32_t* block_table, int max_pages,
                                          const int32_t* kv_len, const int32_t* cu_q, int R,

@@ -10,7 +10,7 @@
 // first rule broken (smallest request, then the rule's order below) as four
 // int32 {code, request, index, value bits}; code 0 means none.  One
 // workgroup walks the requests 256 at a time; it reads only the arrays and
-// sizes it is given.
+// sizes it is given.  (How often a page is named is counted by several, after it.)
 #include "device_common.h"
 #include "kernels.h"
 
@@ -208,10 +208,71 @@ __global__ __launch_bounds__(kChkThreads) void chk_pages(const int32_t* block_ta
     if (!done && threadIdx.x == 0) report[0] = report[1] = report[2] = report[3] = 0;
 }
 
+// Where chk_pages found nothing: 4 a page whose ref is below the number of held entries
+// that name it (the first request that holds such a page; index: logical page, value: the
+// entry).  A workgroup counts kHeldPages pages' entries in LDS, over all requests.  The
+// report collects the smallest request in its second word, then that one's smallest
+// logical page in its third, in three launches:
+enum Held { kHeldOpen, kHeldRequest, kHeldIndex };
+constexpr int kHeldThreads = 1024, kHeldWaves = kHeldThreads / DSPARK_WAVE;
+constexpr int kHeldPages = 8192;
+constexpr int kNoRequest = 0x7fffffff;
+template <Held What>
+__global__ __launch_bounds__(kHeldThreads) void chk_held(const int32_t* block_table, int max_pages, const int32_t* kv_len,
+                                                         int R, int page_size, const int32_t* ref, int num_pages,
+                                                         int32_t* report) {
+    if (report[0]) return;
+    if (What == kHeldOpen) {
+        if (threadIdx.x == 0) report[1] = report[2] = kNoRequest;
+        return;
+    }
+    const int only = What == kHeldIndex ? report[1] : -1;
+    if (only == kNoRequest) return;
+    __shared__ int count[kHeldPages];
+    const int first = blockIdx.x * kHeldPages, n = min(kHeldPages, num_pages - first);
+    const int lane = threadIdx.x & (DSPARK_WAVE - 1), wave = threadIdx.x / DSPARK_WAVE;
+    for (int i = threadIdx.x; i < n; i += kHeldThreads) count[i] = 0;
+    __syncthreads();
+    // f(request, logical page, page - first) for the held entries that name these pages
+    auto walk = [&](auto f) {
+        for (int r = wave; r < R; r += kHeldWaves) {
+            const int np = (int)(((int64_t)kv_len[r] + page_size - 1) / page_size);  // (chk_pages has seen kv_len)
+            for (int p = lane; p < np; p += DSPARK_WAVE) {
+                const int at = block_table[(int64_t)r * max_pages + p] - first;
+                if ((unsigned)at < (unsigned)n) f(r, p, at);
+            }
+        }
+    };
+    walk([&](int, int, int at) { atomicAdd(&count[at], 1); });
+    __syncthreads();
+    walk([&](int r, int p, int at) {
+        if (count[at] <= ref[first + at]) return;
+        if (What == kHeldRequest) atomicMin(&report[1], r);
+        else if (r == only) atomicMin(&report[2], p);
+    });
+}
+__global__ void chk_held_report(const int32_t* block_table, int max_pages, int32_t* report) {
+    if (threadIdx.x || report[0]) return;
+    const int r = report[1], p = report[2];
+    const bool none = r == kNoRequest;
+    report[0] = none ? 0 : 4;
+    report[1] = none ? 0 : r;
+    report[2] = none ? 0 : p;
+    report[3] = none ? 0 : block_table[(int64_t)r * max_pages + p];
+}
+
 hipError_t launch_check_pages(const int32_t* block_table, int max_pages, const int32_t* kv_len, int R, int page_size,
                               const int32_t* ref, int num_pages, int32_t* report, hipStream_t s) {
     hipLaunchKernelGGL(chk_pages, dim3(1), dim3(kChkThreads), 0, s, block_table, max_pages, kv_len, R, page_size, ref,
                        num_pages, report);
+    const dim3 chunks((unsigned)((num_pages + kHeldPages - 1) / kHeldPages)), threads(kHeldThreads);
+    hipLaunchKernelGGL(chk_held<kHeldOpen>, dim3(1), dim3(DSPARK_WAVE), 0, s, block_table, max_pages, kv_len, R, page_size,
+                       ref, num_pages, report);
+    hipLaunchKernelGGL(chk_held<kHeldRequest>, chunks, threads, 0, s, block_table, max_pages, kv_len, R, page_size, ref,
+                       num_pages, report);
+    hipLaunchKernelGGL(chk_held<kHeldIndex>, chunks, threads, 0, s, block_table, max_pages, kv_len, R, page_size, ref,
+                       num_pages, report);
+    hipLaunchKernelGGL(chk_held_report, dim3(1), dim3(DSPARK_WAVE), 0, s, block_table, max_pages, report);
     return hipGetLastError();
 }
 

@@ -196,7 +196,8 @@ CHECK_RULES = {
     "schedule": {1: "confidence outside [0, 1]"},
     "draft": {1: "temperature not finite and positive", 2: "uniform outside [0, 1)"},
     "pages": {1: "kv_len outside [0, max_pages * page_size]", 2: "held table entry outside the cache",
-              3: "held table entry names a page without holders"},
+              3: "held table entry names a page without holders",
+              4: "held table entry names a page that more entries name than its ref"},
 }
 
 
