@@ -422,7 +422,7 @@ size_t dspark_verify_attn_scaled_workspace_size(int R, int max_q, int Hq, int Hk
         return 0;
     dspark::AttnArgs a = make_attn(nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, max_pages, nullptr, nullptr, R,
                                    max_q, Hq, Hkv, Dqk, Dv, page_size, 1.0f, dt, nullptr, nullptr);
-    const size_t need = dspark::attn_generic_workspace(a);
+    const size_t need = dspark::attn_generic_scaled_workspace(a);
     return dspark::attn_scaled_shape_ok(a) ? std::max(need, dspark::attn_scaled_workspace(a)) : need;
 }
 
@@ -450,7 +450,7 @@ dspark_status dspark_verify_attn_scaled(const void* q, const void* k_cache, cons
                                          R, max_q, Hq, Hkv, Dqk, Dv, page_size, scale, dt, out, lse);
     const dspark::CacheScales c = {k_scale, v_scale, block, num_pages};
     // (a call is refused alike whatever its strides and alignment, which decide the kernels)
-    size_t need = dspark::attn_generic_workspace(a);
+    size_t need = dspark::attn_generic_scaled_workspace(a);
     if (dspark::attn_scaled_shape_ok(a)) need = std::max(need, dspark::attn_scaled_workspace(a));
     if (ws_bytes < need || (need > 0 && !ws) || !aligned(ws, 256))
         return fail(DSPARK_EWORKSPACE, "workspace of %zu bytes (256-aligned) needed, got %zu", need, ws_bytes);

@@ -65,6 +65,7 @@ bool attn_scaled_shape_ok(const AttnArgs& a);                          // shape 
 bool attn_scaled_supported(const AttnArgs& a, const CacheScales& c);  // shape and alignment
 size_t attn_scaled_workspace(const AttnArgs& a);
 hipError_t launch_attn_scaled(const AttnArgs& a, const CacheScales& c, void* ws, hipStream_t s);
+size_t attn_generic_scaled_workspace(const AttnArgs& a);
 hipError_t launch_attn_generic_scaled(const AttnArgs& a, const CacheScales& c, void* ws, hipStream_t s);
 
 struct AppendArgs {
