@@ -276,7 +276,7 @@ dspark_status dspark_verify_attn(const void* q, const void* k_cache, const void*
  *     aligned, Dqk and Dv multiples of 16, page_size below 2^20 and fewer than
  *     2^32 scales: matrix cores, HBM-bound.  The codes are widened exactly.  bf16
  *     queries enter as they are, a probability times its value's scale rounded
- *     once to fp16 (2^-11; products below 2^-21 of a row's largest lose bits: rows
+ *     once to fp16 (2^-11; products below 2^-25 of a row's largest lose bits: rows
  *     where that could exceed 2^-9 of their largest value, because what is most
  *     probable has values near zero for its scale, are computed again in fp32, as
  *     are those with non-finite sums, at many times the cost);

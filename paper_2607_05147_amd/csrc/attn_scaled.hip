@@ -69,20 +69,21 @@ constexpr float kLn2 = 0.6931471805599453f;
 // A row's reference m: its exponents are relative to it.  It moves when one exceeds it by
 // kHead, to kBias below that.  fp32: of the scores, p is at most 2^8.  bf16 queries: of
 // the scores + log2 |s_v|, so that p * s_v, which fp16 holds, is at most 2^15 and of full
-// precision down to 2^-21 of the row's largest (fp16 is normal from 2^-14); p alone is
+// precision down to 2^-25 of the row's largest (fp16 is normal from 2^-14); p alone is
 // fp32 (scales outside 2^-100 .. 2^100 count as those; larger ones overflow, and their rows
-// are computed again).
+// are computed again).  2^4 is what a row's largest product may grow until its reference
+// moves; with 2^8 (kBias 7) no call was more than 1 % faster.
 template <bool F32> struct Ref {
-    static constexpr float kBias = F32 ? 0.0f : 7.0f, kHead = F32 ? 8.0f : 15.0f;
+    static constexpr float kBias = F32 ? 0.0f : 11.0f, kHead = F32 ? 8.0f : 15.0f;
 };
 constexpr float kMaxLog = 100.0f;
 // Where the largest p * s_v goes with values near zero, what counts may be what fp16 rounds
-// to multiples of 2^-24: an error of at most 2^-25 a key, times a code of at most 448.  A
-// row whose largest sum is below kLeast for every key of its range, where that error could
-// exceed 2^-9 of it, is computed again.  (A key with p * s_v of 2^7 and a code of 1 in any
-// dim is enough for 18000 keys.)
-constexpr float kLeast = 448.0f / (1 << 16);
-constexpr int kNotFinite = 1, kLow = 2;  // why rows are computed again
+// to multiples of 2^-24: an error of at most 2^-25 a key, times the largest code.  So a row
+// is computed again where a code of its range is above kFine of the row's largest sum by the
+// range's keys: there the error could exceed 2^-9 of that sum.  (A key with p * s_v of 2^11
+// and a value of 1 is enough for 299000 keys, whatever the others' codes.)
+constexpr float kFine = 65536.0f;
+constexpr float kMaxCode = 448.0f;
 constexpr int kMinUnits = 4;         // steps per wave, at least
 constexpr int kPageRegs = 2;         // page ids per lane: 128 pages of a range at a time
 constexpr int kMaxD = 256;
@@ -221,12 +222,13 @@ __device__ __forceinline__ int place(int wave) {
 // products came out non-finite or too low for their roundings: a product over 16 rows and
 // 32 keys also multiplies the keys that a row does not see, by a probability of 0, and 0
 // times a non-finite value is NaN.  Every row takes only its own keys here, as the
-// vector-ALU kernels do.  `why`: if only kLow, values that are all zeros need nothing (a
-// cache that was never filled takes a look at its values, not this).
+// vector-ALU kernels do.  Codes up to `fine` need nothing (below 0: rows are not finite):
+// a look at the values goes first, which a cache of zeros or of small values under a
+// scale of 1 pays alone.
 template <bool F32, int CH, int W, int T>
 __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const int g, const int rc, const int q0,
                                             const int ql, const int kv, const int s0, const int s1, const int ns,
-                                            const int64_t slot, const int why) {
+                                            const int64_t slot, const float fine) {
     typedef Cfg<F32, CH, W, T> C;
     typedef typename std::conditional<F32, float, uint16_t>::type E;
     constexpr int kPer = (C::Dp + DSPARK_WAVE - 1) / DSPARK_WAVE;  // value dims per lane
@@ -243,16 +245,20 @@ __device__ __forceinline__ void scaled_rows(const Params& p, const int r, const 
     const uint8_t* vc = (const uint8_t*)a.v + gv * p.vs1;
     const bool whole = s0 + z == 0 && s1 == ns;
     float* part = p.part + (slot + z) * ((int64_t)C::Rows * (C::Dp + 2));
-    if (!F32 && !(why & kNotFinite)) {
+    if (!F32 && fine >= 0.0f) {
         const int end = min(kv, s1 * C::Step);
         bool some = false;
         for (int k0 = (s0 + z) * C::Step; k0 < end && !some; k0 += DSPARK_WAVE) {
             const int key = min(k0 + lane, end - 1), at = key % page;
             const int64_t pg = clamp_page(p, bt[key / page]);
             const u32x4* vr = (const u32x4*)(vc + pg * p.vs0 + (int64_t)at * p.vs2);
-            uint32_t bits = 0;
-            for (int d = 0; d < a.Dv / 16 + z; ++d) bits |= (vr[d][0] | vr[d][1] | vr[d][2] | vr[d][3]) & 0x7f7f7f7fu;
-            some = __builtin_amdgcn_ballot_w64(bits && p.cs.v[(pg * a.Hkv + gv) * p.nb + at / p.cs.block] != 0.0f) != 0;
+            uint32_t most = 0;  // (magnitudes of codes are in the order of their bits)
+            for (int d = 0; d < a.Dv / 16 + z; ++d) {
+                const u32x4 x = vr[d];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) most = max(most, x[e >> 2] >> (8 * (e & 3)) & 0x7fu);
+            }
+            some = __builtin_amdgcn_ballot_w64(!(e4m3_to_f32(most) <= fine) && p.cs.v[(pg * a.Hkv + gv) * p.nb + at / p.cs.block] != 0.0f) != 0;
         }
         if (!some) return;
     }
@@ -502,15 +508,15 @@ struct Tiles {
         }
     }
 
-    // The rows' results, or their partials, over `keys` keys.  Returns why they have to be
-    // computed again, if so (what is written is then not yet the result).
-    __device__ __forceinline__ int finish(const Params& p, int g, int row0, int first, int q0, int ql, bool whole,
-                                          float* part, int keys) {
+    // The rows' results, or their partials, over `keys` keys.  Returns the code up to which
+    // they are precise, below 0 where a sum is not finite (what is written is then not yet the
+    // result).
+    __device__ __forceinline__ float finish(const Params& p, int g, int row0, int first, int q0, int ql, bool whole,
+                                            float* part, int keys) {
         const AttnArgs& a = p.a;
         const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
-        const float least = kLeast * (float)keys;
         float most = 0.0f;  // largest sum by magnitude (NaN if one is)
-        bool low = false;
+        float least = __builtin_huge_valf();  // largest sum of the row where that is the least
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             // total l over the four lanes of a row
@@ -527,7 +533,7 @@ struct Tiles {
             const int row = first + 16 * W * j + lr, rr = row - row0;
             if (row >= ql * p.group) continue;
             most = vmax(vmax(big[0], l[j]), most);
-            if constexpr (!F32) low = low || (l[j] > 0.0f && big[1] < least);
+            if (!F32 && l[j] > 0.0f) least = fminf(least, big[1]);
             const int t = row / p.group;
             const int64_t orow = (int64_t)(q0 + t) * a.Hq + g * p.group + (row - t * p.group);
             float inv = 1.0f / l[j];
@@ -553,8 +559,8 @@ struct Tiles {
                 }
             }
         }
-        return (__builtin_amdgcn_ballot_w64(!(most < __builtin_huge_valf())) ? kNotFinite : 0) |
-               (__builtin_amdgcn_ballot_w64(low) ? kLow : 0);
+        if (__builtin_amdgcn_ballot_w64(!(most < __builtin_huge_valf()))) return -1.0f;
+        return F32 ? __builtin_huge_valf() : kFine / (float)keys * -wave_max(-least);
     }
 };
 
@@ -594,9 +600,9 @@ struct Reads {
 // Steps [s0, s1) of the ns steps of one (request, head, chunk) of N row tiles, by a single
 // wave.  `slot`: where the partial goes when they are not all of them.
 template <bool F32, int CH, int T, int N>
-__device__ __forceinline__ int attend(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
-                                      const int q0, const int ql, const int kv, const int s0, const int s1,
-                                      const int ns, const int64_t slot) {
+__device__ __forceinline__ float attend(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
+                                        const int q0, const int ql, const int kv, const int s0, const int s1,
+                                        const int ns, const int64_t slot) {
     typedef Cfg<F32, CH, 1, T> C;
     constexpr int S = C::S, H = C::H, P = C::P;
     const AttnArgs& a = p.a;
@@ -747,9 +753,9 @@ __device__ __forceinline__ int attend(const Params& p, const uint32_t lds0, cons
 // none).  Each wave copies its part of a step, Ring - 1 steps ahead, into a ring of
 // buffers; one barrier a step.
 template <bool F32, int CH, int W, int T, int N>
-__device__ __forceinline__ int attend_shared(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
-                                             const int q0, const int ql, const int kv, const int s0, const int s1,
-                                             const int ns, const int64_t slot) {
+__device__ __forceinline__ float attend_shared(const Params& p, const uint32_t lds0, const int r, const int g, const int rc,
+                                               const int q0, const int ql, const int kv, const int s0, const int s1,
+                                               const int ns, const int64_t slot) {
     typedef Cfg<F32, CH, W, T> C;
     constexpr int S = C::S, H = C::H, P = C::P, R = C::Ring;
     constexpr int kOps = P * S / W;  // copies of a wave for a step's keys, and for its values
@@ -867,7 +873,7 @@ __device__ __forceinline__ int attend_shared(const Params& p, const uint32_t lds
     if constexpr (N > 0)
         return tiles.finish(p, g, row0, first, q0, ql, s0 == 0 && s1 == ns,
                             p.part + slot * ((int64_t)C::Rows * (C::Dp + 2)), (s1 - s0) * C::Step);
-    return 0;
+    return __builtin_huge_valf();
 }
 
 template <bool F32, int CH, int W, int T>
@@ -879,7 +885,7 @@ void attn_scaled_kernel(Params p) {
     if (C::Group > 1) lds0 += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * C::LdsB;
     asm volatile("" : "+s"(lds0));
     const int wave = place<W>(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
-    int again = 0;
+    float fine = __builtin_huge_valf();  // codes up to this need no second look
     range_walk<C::Step, true, C::Group>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
         // (a body for each number of tiles: tests of it would cut the step into pieces that
         // the compiler cannot interleave)
@@ -887,19 +893,19 @@ void attn_scaled_kernel(Params p) {
         const int mine = (n - wave + W - 1) / W;                // dealt round-robin
         if constexpr (W == 1) {
             if constexpr (T > 1)
-                if (mine > 1) return (void)(again |= attend<F32, CH, T, 2>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot));
-            again |= attend<F32, CH, T, 1>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
+                if (mine > 1) return (void)(fine = fminf(fine, attend<F32, CH, T, 2>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot)));
+            fine = fminf(fine, attend<F32, CH, T, 1>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot));
         } else {
-            if (mine > 0) again |= attend_shared<F32, CH, W, T, 1>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
+            if (mine > 0) fine = fminf(fine, attend_shared<F32, CH, W, T, 1>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot));
             else attend_shared<F32, CH, W, T, 0>(p, lds0, r, g, rc, q0, ql, kv, s0, s1, ns, slot);
         }
     });
-    if (!again) return;
+    if (fine >= kMaxCode) return;
     // (a walk of its own, so that the step loop above holds none of its registers; a wave
     // goes over its own rows only)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what the lanes wrote above comes before what others write below
     range_walk<C::Step, true, C::Group>(p, [&](int r, int g, int rc, int q0, int ql, int kv, int s0, int s1, int ns, int64_t slot) {
-        scaled_rows<F32, CH, W, T>(p, r, g, rc, q0, ql, kv, s0, s1, ns, slot, again);
+        scaled_rows<F32, CH, W, T>(p, r, g, rc, q0, ql, kv, s0, s1, ns, slot, fine);
     });
 }
 

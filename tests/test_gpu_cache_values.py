@@ -83,10 +83,21 @@ def test_values_that_are_all_zeros_of_any_scale(group, dt):
     assert (o == 0).all()
 
 
-@pytest.mark.parametrize("below", [20, 22, 24, 26])
+@pytest.mark.parametrize("size", [0.003, 0.05])
+@pytest.mark.parametrize("group,D", [(2, 64), (9, 64), (8, 128), (12, 256)])
+def test_small_values_under_one_scale(group, D, size):
+    c = Case([5, 2, 1], [2100, 130, 40], 2 * group, 2, D, D, 16, 16, torch.bfloat16, seed=44)
+    c.code["v"] = np.where(c.code["v"] == 0x7f, 0x7f, e4m3(c.rng.normal(0, size, c.code["v"].shape)))
+    c.scale["v"][:] = np.where(np.isnan(c.scale["v"]), np.nan, np.float32(1.0))
+    q = torch.from_numpy(c.rng.normal(0, 1, (c.rows, c.Hq, D)).astype(np.float32)).to(c.dt).to(dev())
+    out, lse = attend(c, c.on_device(), q)
+    check_attention(c, q, out, lse)
+
+
+@pytest.mark.parametrize("below", [20, 22, 24, 26, 28, 30])
 def test_values_far_below_the_rows_largest(below):
-    # a value of 448 in one dim, and a block whose p * s is 2^-below of that token's: subnormal in
-    # fp16, whose error is 2^-25 of 448 times (at most 64 tokens' codes of at most 448) in absolute terms
+    # values of 448 in one dim, and blocks whose p * s is 2^-below of those tokens': subnormal in fp16
+    # at last, an error of 2^-25 where that is 2^7 or more, for 64 tokens' codes of at most 448
     c = Case([1], [64 + 16], 1, 1, 64, 64, 16, 16, torch.bfloat16, seed=43)
     q = torch.ones(1, 1, 64, dtype=torch.bfloat16, device=dev())
     c.code["k"][:] = 0
