@@ -968,7 +968,8 @@ static Geom geom(const AttnArgs& a) {
     //    fp32, 64          48 / 41   66 / 56   77 / 78  126 / 115  60 / 50   76 / 77   185 / 181
     //    fp32, 128        100 / 70  109 / 91  118 / 140 208 / 238 109 / 79  121 / 147  317 / 418
     //    fp32, 256        270 / 127 279 / 176 292 / 263 534 / 462 274 / 147 292 / 272  804 / 793
-    // (8 requests of 500-1000 keys, fp32, 64: four 1.5 to 6 us the shorter.)
+    // (fp32 heads of 64 take four waves above 32 rows although one is 4 to 11 us the shorter
+    // for 48 requests of 68 rows or more: with 8 of 500-1000 keys four are 1.5 to 6 us the shorter, more of a call.)
     // 32 of at most 32 rows, another batch: bf16 168 / 145, 147 / 142 and 141 / 188.
     // Two tiles a wave of four, 128 requests of 64/8 heads: 136 rows each 650 against
     // 780, but 324 against 283 where a request has 35 on average.  Short contexts are

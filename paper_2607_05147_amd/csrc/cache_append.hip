@@ -20,7 +20,8 @@
 // an address and a mask a pass (151 registers, three waves a SIMD instead of five).
 //
 // Bound by launch and three dependent loads at a step's sizes (565 rows of 8 heads:
-// 7.0 us), by HBM for prompts: 40000 rows of 8 heads of 128, 246 MB, 70 us, 3.5 TB/s.
+// 7.0 us).  Prompts: 40000 rows of 8 heads of 128, 246 MB, 70 us, 3.5 TB/s; a wave's loads,
+// maximum and stores follow each other, and workgroups of a grid for max_q find no rows.
 #include <algorithm>
 #include <type_traits>
 
