@@ -1,7 +1,7 @@
 """GPU tests of dspark_verify_attn_scaled where a worker's range of keys is longer than the 128 pages
 whose ids it holds: it reads the next ids and starts its copies again in the middle of the range.
 
-A card's workers, 1024 to 3072 of them, share a batch's keys equally, so the batch has to have
+A card's workers, 4 to 12 of a CU, share a batch's keys equally, so the batch has to have
 millions; requests name the pages of a small pool again and again.  Tolerances are those of
 test_gpu_cache.py: scores of a standard deviation of 2 leave a row's sum of 100000 values as
 much weight as 2000 equally probable ones, and its rounding errors are random as theirs.
