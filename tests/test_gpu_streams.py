@@ -131,3 +131,21 @@ def test_results_read_on_the_current_stream_live_until_it_has_read_them():
     assert other.data_ptr() != at
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def test_a_captured_call_on_a_side_stream_that_allocates():
+    c = Case([3, 1], [300, 90], 16, 2, 128, 128, 64, 64, torch.bfloat16, seed=19)
+    d, q = c.on_device(), queries(c)
+    want, want_lse = attend(c, d, q)
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s.wait_stream(torch.cuda.current_stream())
+        out, lse = dspark.dspark_verify_attn_scaled(q, d["kc"], d["vc"], c.strides["k"], c.strides["v"], d["ks"], d["vs"], c.block, d["table"],
+                                                    d["kv"], d["cu"], c.max_q, c.Dv, c.page, c.Dqk ** -0.5, want_lse=True, stream=s)
+        torch.cuda.current_stream().wait_stream(s)
+    for _ in range(3):
+        out.zero_(), lse.zero_()
+        float((q.float() * q.float()).sum())  # eager work and a synchronization between replays
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
