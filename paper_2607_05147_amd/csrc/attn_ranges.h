@@ -178,7 +178,8 @@ __device__ __forceinline__ void range_walk(const Ranges& p, F f) {
 // against 8: 4 requests of up to 136 rows, 8-bit cache 40.5 and 42.6, bf16 heads of 128
 // 35.9 and 38.6, fp32 107 and 112; but 8 requests of up to 520 rows, fp32 heads of 64,
 // 33.1 and 29.7 (16 parts 29.6), 16 requests 42.0 and 39.2: with more of its workgroups
-// the next call's attention is the slower one.  Fewer than 8 gain nothing (128 requests
+// the next call's attention is the slower one.  (bf16 heads of 128, 32 requests of up to 264
+// rows, would gain: 16 parts 36.7, 8 parts 38.7.)  Fewer than 8 gain nothing (128 requests
 // 272 and 273, 1024 and 2048 the same).
 constexpr int kMergeThreads = 256;
 constexpr int kMergeBatch = 8;
